@@ -354,7 +354,7 @@ def run(state):
     if c["kind"] == "dropout":
         return {"y": layers.dropout(s["x"], drop), "dx": layers.dropout(s["dy"], drop)}
     how = dict(row_begin=s["row_begin"], index=s["index"], norm=c["norm"] if c["post"] else None, post=s["post"],
-               gate=s["gamma"] if s["gamma"] is not None else s["z"], scale=c["scale"], drop=drop,
+               gate=s["gamma"], gate_logits=s["z"], scale=c["scale"], drop=drop,
                next_norm=c["norm"] if c["pre"] else None, pre=s["pre"], eps=EPS)
     out = {}
     out["y"], h = layers.residual(s["x"], s["b"], **how)
@@ -363,7 +363,7 @@ def run(state):
     if c["train"]:
         back = layers.residual_grad(s["dy"], s["dh"], s["y"], s["b"], **how)
         out["dx"], out["db"] = back.dx, back.db
-        for name, grad in (("dpost", back.dpost), ("dpre", back.dpre), ("dgamma" if s["z"] is None else "dz", back.dgate)):
+        for name, grad in (("dpost", back.dpost), ("dpre", back.dpre), ("dgamma", back.dgate), ("dz", back.dlogits)):
             if grad is not None:
                 out[name] = grad
     return out
