@@ -32,7 +32,10 @@ def build_library():
     os.makedirs(OBJ, exist_ok=True)
     objs = []
     for src, extra in (("hop_kernels.hip", DEVICE),
+                       ("hop_product.hip", DEVICE),
+                       ("hop_residual.hip", DEVICE),
                        ("hop_api.cpp", []),
+                       ("hop_layers.cpp", []),
                        ("hop_sim.cpp", ["-ffp-contract=off"])):
         o = os.path.join(OBJ, src + ".o")
         _run([hipcc] + COMMON + extra + ["-c", os.path.join(CSRC, src), "-o", o])
