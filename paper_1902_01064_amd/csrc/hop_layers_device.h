@@ -109,6 +109,21 @@ __device__ __forceinline__ bool find_piece(const HopRows& rows, int shift, int p
     return false;
 }
 
+// How many pieces of 1 << shift rows there are.
+__device__ __forceinline__ int count_pieces(const HopRows& rows, int shift) {
+    const int step = 1 << shift;
+    if (!rows.begin) return (int)(((int64_t)rows.rows + step - 1) >> shift);
+    const HOPL_GLOBAL int32_t* table = (const HOPL_GLOBAL int32_t*)rows.begin;
+    int n = 0;
+    for (int g = threadIdx.x & 63; g < rows.G; g += 64) {
+        const int b = clamp_int(table[g], 0, rows.rows), e = clamp_int(table[g + 1], b, rows.rows);
+        n += (int)(((int64_t)(e - b) + step - 1) >> shift);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
 // The rows of group g.
 __device__ __forceinline__ void group_rows(const HopRows& rows, int g, int* b, int* e) {
     if (!rows.begin) {
