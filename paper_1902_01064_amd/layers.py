@@ -67,41 +67,57 @@ def load():
 
 
 # ------------------------------------------------------------------------------------------ arguments ----
-def _ld(t, name, dtype, shape=None):
-    """Distance between the rows of a matrix."""
-    if t.dim() != 2 or (shape is not None and t.shape != shape):
-        raise ValueError("%s: a matrix %s is needed, got %s" % (name, "" if shape is None else list(shape), list(t.shape)))
-    if t.dtype != dtype:
-        raise TypeError("%s: %s is needed, got %s" % (name, dtype, t.dtype))
-    if not t.is_cuda:
+# A kernel of a small call takes less time than its launch (4 us), so what is asked of the arguments is asked in the order that lets plain
+# ones through with few questions, and devices are compared as numbers.
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _rows(x, name):
+    """(type, GPU, distance between rows, rows, columns) of the tensor that a call goes by."""
+    try:
+        dtype = _TYPES[x.dtype]
+    except KeyError:
+        raise TypeError("%s: float32 or bfloat16 is needed, got %s" % (name, x.dtype)) from None
+    gpu = x.get_device()
+    if gpu < 0:
         raise ValueError("%s: a tensor on the GPU is needed" % name)
-    rows, cols = t.shape
+    if gpu != torch.cuda.current_device():
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, gpu, torch.cuda.current_device()))
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError("%s: a matrix is needed, got %s" % (name, list(shape)))
+    return dtype, gpu, _distance(x, name, shape[0], shape[1]), shape[0], shape[1]
+
+
+def _distance(t, name, rows, cols):
     ld, step = t.stride()
-    if rows == 0:
-        return cols
+    if step == 1 and ld >= cols or rows == 0:
+        return ld if ld >= cols else cols
     if cols > 1 and step != 1:
         raise ValueError("%s: columns have to be contiguous, got strides %s" % (name, list(t.stride())))
-    if rows == 1:
-        return max(ld, cols)
-    if ld < cols:
+    if rows > 1 and ld < cols:
         raise ValueError("%s: rows overlap, got strides %s" % (name, list(t.stride())))
-    return ld
+    return max(ld, cols)
 
 
-def _type(t, name):
-    try:
-        return _TYPES[t.dtype]
-    except KeyError:
-        raise TypeError("%s: float32 or bfloat16 is needed, got %s" % (name, t.dtype)) from None
+def _ld(t, name, dtype, gpu, rows, cols):
+    """Distance between the rows of a matrix that has to be rows x cols."""
+    if t.shape != (rows, cols):
+        raise ValueError("%s: a matrix [%d, %d] is needed, got %s" % (name, rows, cols, list(t.shape)))
+    if t.dtype is not dtype:
+        raise TypeError("%s: %s is needed, got %s" % (name, dtype, t.dtype))
+    if t.get_device() != gpu:
+        raise ValueError("%s: a tensor on cuda:%d is needed" % (name, gpu))
+    return _distance(t, name, rows, cols)
 
 
-def _table(row_begin, device):
+def _table(row_begin, gpu):
     """(address, G) of a row table."""
     if row_begin is None:
         return 0, 1
-    if row_begin.dtype != torch.int32 or row_begin.dim() != 1 or row_begin.numel() < 2 or not row_begin.is_contiguous() or row_begin.device != device:
-        raise ValueError("row_begin: a contiguous int32 vector of G + 1 row numbers on %s is needed" % device)
-    return row_begin.data_ptr(), row_begin.numel() - 1
+    if row_begin.dtype is not torch.int32 or row_begin.get_device() != gpu or row_begin.dim() != 1 or row_begin.shape[0] < 2 or row_begin.stride(0) != 1:
+        raise ValueError("row_begin: a contiguous int32 vector of G + 1 row numbers on cuda:%d is needed" % gpu)
+    return row_begin.data_ptr(), row_begin.shape[0] - 1
 
 
 def _index(index, G, M, name):
@@ -119,36 +135,29 @@ def _address(a):
     return 0 if a is None else a.buffer_info()[0]
 
 
-def _vector(t, name, cols, device, M=None):
+def _vector(t, name, cols, gpu, M=None):
     """(address, distance, M) of a parameter [M, cols] in float32."""
     if t is None:
         return 0, 0, M
-    if t.dim() != 2 or t.shape[1] != cols or t.dtype != torch.float32 or t.device != device or (cols > 1 and t.stride(1) != 1):
-        raise ValueError("%s: float32 [groups, %d] with contiguous columns on %s is needed" % (name, cols, device))
-    if M is not None and t.shape[0] != M:
-        raise ValueError("%s: %d rows, other parameters have %d" % (name, t.shape[0], M))
-    return t.data_ptr(), t.stride(0), t.shape[0]
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != cols or t.dtype is not torch.float32 or t.get_device() != gpu or (cols > 1 and t.stride(1) != 1):
+        raise ValueError("%s: float32 [groups, %d] with contiguous columns on cuda:%d is needed" % (name, cols, gpu))
+    if M is not None and shape[0] != M:
+        raise ValueError("%s: %d rows, other parameters have %d" % (name, shape[0], M))
+    return t.data_ptr(), t.stride(0), shape[0]
 
 
-def _weights(w, name, device):
-    if w.dim() != 3 or w.device != device or (w.shape[2] > 1 and w.stride(2) != 1) or (w.shape[1] > 1 and w.stride(1) < w.shape[2]):
-        raise ValueError("%s: [groups, rows, columns] with contiguous columns on %s is needed, got %s with strides %s"
-                         % (name, device, list(w.shape), list(w.stride())))
-    return max(w.stride(1), w.shape[2])
+def _weights(w, name, gpu):
+    """(distance between groups, distance between rows, shape) of [M, rows, columns]."""
+    shape, stride = w.shape, w.stride()
+    if len(shape) != 3 or w.get_device() != gpu or (shape[2] > 1 and stride[2] != 1) or (shape[1] > 1 and stride[1] < shape[2]):
+        raise ValueError("%s: [groups, rows, columns] with contiguous columns on cuda:%d is needed, got %s with strides %s"
+                         % (name, gpu, list(shape), list(stride)))
+    return stride[0], max(stride[1], shape[2]), shape
 
 
-def _stream(t):
-    return torch.cuda.current_stream(t.device).cuda_stream
-
-
-def _on(t):
-    """Kernels run on the tensors' GPU, whichever is the current one."""
-    if torch.cuda.current_device() != t.device.index:
-        raise ValueError("tensors are on %s, the current device is cuda:%d" % (t.device, torch.cuda.current_device()))
-
-
-def _scratch(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _scratch(nbytes, like):
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
 def _drop(drop):
@@ -163,91 +172,93 @@ def _at(packed):
 def product(x, w, row_begin=None, index=None, transposed=False, out=None):
     """y[r] = w_g x[r] for the rows r of group g; w [M, out, in].  transposed: y[r] = w_g^T x[r] - the gradient to x from
     one to y, with the same w."""
-    lib, dtype = load(), _type(x, "x")
-    ldx = _ld(x, "x", x.dtype)
-    rows, k = x.shape
-    table, G = _table(row_begin, x.device)
-    ldw = _weights(w, "w", x.device)
-    if w.dtype != x.dtype or w.shape[1 if transposed else 2] != k:
+    dtype, gpu, ldx, rows, k = _rows(x, "x")
+    table, G = _table(row_begin, gpu)
+    step, ldw, (M, a, b) = _weights(w, "w", gpu)
+    if transposed:
+        a, b = b, a
+    if w.dtype is not x.dtype or b != k:
         raise ValueError("w: %s [groups, %s] is needed, got %s %s" % (x.dtype, "%d, out" % k if transposed else "out, %d" % k, w.dtype, list(w.shape)))
-    n = w.shape[2 if transposed else 1]
-    idx = _index(index, G, w.shape[0], "w")
+    idx = _index(index, G, M, "w")
     if out is None:
-        out = torch.empty((rows, n), dtype=x.dtype, device=x.device)
-        ldy = n
+        out, ldy = x.new_empty((rows, a)), a
     else:
-        ldy = _ld(out, "out", x.dtype, (rows, n))
-    _on(x)
-    a = _PRODUCT(rows, table, G, dtype, x.data_ptr(), ldx, w.data_ptr(), ldw, w.stride(0), _address(idx), out.data_ptr(), ldy, k, n,
-                 1 if transposed else 0, 0)
-    need = lib.hop_product_scratch_bytes(a)
-    s = _scratch(need, x.device)
-    hop._check(lib.hop_product(a, s.data_ptr() if need else None, need, _stream(x)), "hop_product")
+        ldy = _ld(out, "out", x.dtype, gpu, rows, a)
+    args = _PRODUCT(rows, table, G, dtype, x.data_ptr(), ldx, w.data_ptr(), ldw, step, _address(idx), out.data_ptr(), ldy, k, a,
+                    1 if transposed else 0, 0)
+    lib = load()
+    need = lib.hop_product_scratch_bytes(args)
+    s = _scratch(need, x)
+    hop._check(lib.hop_product(args, s.data_ptr() if need else None, need, _raw_stream(gpu)), "hop_product")
     return out
 
 
 def product_grad(dy, x, row_begin=None, out=None, index=None):
     """dw_g = sum over the group's rows of dy[r] x[r]^T, in float32: [G, out, in], or into the rows `index` of `out`."""
-    lib, dtype = load(), _type(x, "x")
-    lddy, ldx = _ld(dy, "dy", x.dtype), _ld(x, "x", x.dtype)
-    if dy.shape[0] != x.shape[0]:
-        raise ValueError("dy has %d rows, x %d" % (dy.shape[0], x.shape[0]))
-    (rows, n), k = dy.shape, x.shape[1]
-    table, G = _table(row_begin, x.device)
+    dtype, gpu, ldx, rows, k = _rows(x, "x")
+    if dy.dim() != 2 or dy.shape[0] != rows:
+        raise ValueError("dy: a matrix of x's %d rows is needed, got %s" % (rows, list(dy.shape)))
+    n = dy.shape[1]
+    lddy = _ld(dy, "dy", x.dtype, gpu, rows, n)
+    table, G = _table(row_begin, gpu)
     if out is None:
         if index is not None:
             raise ValueError("index without out")
-        out = torch.empty((G, n, k), dtype=torch.float32, device=x.device)
-    elif out.dtype != torch.float32 or out.shape[1:] != (n, k):
+        out = x.new_empty((G, n, k), dtype=torch.float32)
+    elif out.dtype is not torch.float32 or out.shape[1:] != (n, k):
         raise ValueError("out: float32 [groups, %d, %d] is needed, got %s %s" % (n, k, out.dtype, list(out.shape)))
-    lddw = _weights(out, "out", x.device)
-    idx = _index(index, G, out.shape[0], "out")
-    _on(x)
-    a = _PRODUCT_GRAD(rows, table, G, dtype, dy.data_ptr(), lddy, x.data_ptr(), ldx, out.data_ptr(), lddw, out.stride(0), _address(idx), k, n)
-    need = lib.hop_product_grad_scratch_bytes(a)
-    s = _scratch(need, x.device)
-    hop._check(lib.hop_product_grad(a, s.data_ptr() if need else None, need, _stream(x)), "hop_product_grad")
+    step, lddw, (M, _, _) = _weights(out, "out", gpu)
+    idx = _index(index, G, M, "out")
+    args = _PRODUCT_GRAD(rows, table, G, dtype, dy.data_ptr(), lddy, x.data_ptr(), ldx, out.data_ptr(), lddw, step, _address(idx), k, n)
+    lib = load()
+    need = lib.hop_product_grad_scratch_bytes(args)
+    s = _scratch(need, x)
+    hop._check(lib.hop_product_grad(args, s.data_ptr() if need else None, need, _raw_stream(gpu)), "hop_product_grad")
     return out
 
 
 # -------------------------------------------------------------------------------------------- dropout ----
 def dropout(x, drop, out=None):
     """x / (1 - p) where the mask of `drop` keeps it, else 0.  The gradient is dropout(dy, drop)."""
-    dtype = _type(x, "x")
-    ldx = _ld(x, "x", x.dtype)
-    rows, cols = x.shape
+    dtype, gpu, ldx, rows, cols = _rows(x, "x")
     if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-        ldy = cols
+        out, ldy = x.new_empty((rows, cols)), cols
     else:
-        ldy = _ld(out, "out", x.dtype, x.shape)
-    _on(x)
-    hop._check(load().hop_dropout(dtype, x.data_ptr(), ldx, out.data_ptr(), ldy, rows, cols, _drop(drop), _stream(x)), "hop_dropout")
+        ldy = _ld(out, "out", x.dtype, gpu, rows, cols)
+    hop._check(load().hop_dropout(dtype, x.data_ptr(), ldx, out.data_ptr(), ldy, rows, cols, _drop(drop), _raw_stream(gpu)), "hop_dropout")
     return out
 
 
 # ------------------------------------------------------------------------------ norms around a block ----
-def _residual_args(rows, cols, dtype, b, row_begin, index, norm, post, gate, logits, scale, drop, next_norm, pre, eps, device, torch_type):
+def _residual_args(rows, cols, dtype, like, gpu, b, row_begin, index, norm, post, gate, logits, scale, drop, next_norm, pre, eps):
     """(packed hop_residual_args, what has to live as long, G)."""
-    table, G = _table(row_begin, device)
-    ldb = 0 if b is None else _ld(b, "b", torch_type, (rows, cols))
-    post_at, post_step, M = _vector(post, "post", cols, device)
-    pre_at, pre_step, M = _vector(pre, "pre", cols, device, M)
-    gate_at, gate_step, M = _vector(gate, "gate", cols, device, M)
+    table, G = _table(row_begin, gpu)
+    b_at, ldb = (0, 0) if b is None else (b.data_ptr(), _ld(b, "b", like, gpu, rows, cols))
+    post_at, post_step, M = _vector(post, "post", cols, gpu)
+    pre_at, pre_step, M = _vector(pre, "pre", cols, gpu, M)
+    gate_at, gate_step, M = _vector(gate, "gate", cols, gpu, M)
     kind, z_at, ldz = HOP_GATE_NONE if gate is None else HOP_GATE_VECTOR, 0, 0
     if logits is not None:
         if gate is not None:
             raise ValueError("gate and gate_logits: there is one gate")
-        kind, z_at, ldz = HOP_GATE_ELEMENT, logits.data_ptr(), _ld(logits, "gate_logits", torch_type, (rows, cols))
+        kind, z_at, ldz = HOP_GATE_ELEMENT, logits.data_ptr(), _ld(logits, "gate_logits", like, gpu, rows, cols)
     idx = None if M is None else _index(index, G, M, "post, pre, gate")
     packed = _drop(drop)
     try:
         norm, next_norm = _NORMS[norm], _NORMS[next_norm]
     except (KeyError, TypeError):
         raise ValueError("norm: None, 'rms' or 'centred'") from None
-    a = _RESIDUAL(rows, table, G, dtype, cols, 0 if b is None else b.data_ptr(), ldb, z_at, ldz, post_at, post_step, pre_at, pre_step,
-                  gate_at, gate_step, _address(idx), _at(packed), norm, next_norm, kind, scale, eps, 0)
-    return a, (idx, packed), G
+    args = _RESIDUAL(rows, table, G, dtype, cols, b_at, ldb, z_at, ldz, post_at, post_step, pre_at, pre_step, gate_at, gate_step, _address(idx),
+                     _at(packed), norm, next_norm, kind, scale, eps, 0)
+    return args, (idx, packed), G
+
+
+def _result(t, x, name, gpu, rows, cols):
+    """(tensor, address, distance) of a result like x."""
+    if t is None:
+        t = x.new_empty((rows, cols))
+        return t, t.data_ptr(), cols
+    return t, t.data_ptr(), _ld(t, name, x.dtype, gpu, rows, cols)
 
 
 def residual(x, b, row_begin=None, index=None, norm="rms", post=None, gate=None, gate_logits=None, scale=1.0, drop=None, next_norm=None, pre=None, eps=1e-5,
@@ -256,33 +267,23 @@ def residual(x, b, row_begin=None, index=None, norm="rms", post=None, gate=None,
 
     post, pre: [M, cols] float32 or None (1).  The gate is `gate`, [M, cols] float32, as it is; or the logistic function of
     `gate_logits`, a tensor like x; or 1.  norm, next_norm: None, "rms", "centred"."""
-    dtype = _type(x, "x")
-    ldx = _ld(x, "x", x.dtype)
-    rows, cols = x.shape
+    dtype, gpu, ldx, rows, cols = _rows(x, "x")
     if b is None:
         raise ValueError("b: a matrix is needed (norm() is a norm by itself)")
-    a, keep, _ = _residual_args(rows, cols, dtype, b, row_begin, index, norm, post, gate, gate_logits, scale, drop, next_norm, pre, eps, x.device, x.dtype)
-    y = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out
-    ldy = _ld(y, "out", x.dtype, x.shape)
-    h, ldh = None, 0
-    if next_norm is not None:
-        h = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out_next is None else out_next
-        ldh = _ld(h, "out_next", x.dtype, x.shape)
-    _on(x)
-    hop._check(load().hop_residual(a, x.data_ptr(), ldx, y.data_ptr(), ldy, None if h is None else h.data_ptr(), ldh, _stream(x)), "hop_residual")
+    args, keep, _ = _residual_args(rows, cols, dtype, x.dtype, gpu, b, row_begin, index, norm, post, gate, gate_logits, scale, drop, next_norm, pre, eps)
+    y, y_at, ldy = _result(out, x, "out", gpu, rows, cols)
+    h, h_at, ldh = (None, None, 0) if next_norm is None else _result(out_next, x, "out_next", gpu, rows, cols)
+    hop._check(load().hop_residual(args, x.data_ptr(), ldx, y_at, ldy, h_at, ldh, _raw_stream(gpu)), "hop_residual")
     del keep
     return y, h
 
 
 def norm(x, pre=None, row_begin=None, index=None, norm="rms", eps=1e-5, out=None):
     """norm(x) * pre: the norm before a network's first block."""
-    dtype = _type(x, "x")
-    ldx = _ld(x, "x", x.dtype)
-    a, keep, _ = _residual_args(*x.shape, dtype, None, row_begin, index, None, None, None, None, 1.0, None, norm, pre, eps, x.device, x.dtype)
-    h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    ldh = _ld(h, "out", x.dtype, x.shape)
-    _on(x)
-    hop._check(load().hop_residual(a, x.data_ptr(), ldx, None, 0, h.data_ptr(), ldh, _stream(x)), "hop_residual")
+    dtype, gpu, ldx, rows, cols = _rows(x, "x")
+    args, keep, _ = _residual_args(rows, cols, dtype, x.dtype, gpu, None, row_begin, index, None, None, None, None, 1.0, None, norm, pre, eps)
+    h, h_at, ldh = _result(out, x, "out", gpu, rows, cols)
+    hop._check(load().hop_residual(args, x.data_ptr(), ldx, None, 0, h_at, ldh, _raw_stream(gpu)), "hop_residual")
     del keep
     return h
 
@@ -293,26 +294,25 @@ def residual_grad(dy, dh, y, b, row_begin=None, index=None, norm="rms", post=Non
 
     dpost, dpre, dgate: where the parameters' gradients go ([M, cols] float32, written in the rows grad_index), or None for new tensors
     [G, cols].  dx, db, dlogits likewise, like x."""
-    first = dy if dy is not None else dh
-    if first is None:
+    like = dy if dy is not None else dh
+    if like is None:
         raise ValueError("dy and dh are both None")
-    dtype, like, device = _type(first, "dy"), first.dtype, first.device
-    rows, cols = shape = first.shape
+    dtype, gpu, ld, rows, cols = _rows(like, "dy" if dy is not None else "dh")
     if dh is not None and (next_norm is None or y is None):
         raise ValueError("dh needs next_norm and residual's result y")
-    a, keep, G = _residual_args(rows, cols, dtype, b, row_begin, index, norm, post, gate, gate_logits, scale, drop, next_norm, pre, eps, device, like)
-    lddy = 0 if dy is None else _ld(dy, "dy", like)
-    lddh = 0 if dh is None else _ld(dh, "dh", like, shape)
-    ldy = 0 if dh is None else _ld(y, "y", like, shape)
+    args, keep, G = _residual_args(rows, cols, dtype, like.dtype, gpu, b, row_begin, index, norm, post, gate, gate_logits, scale, drop, next_norm, pre, eps)
+    dy_at, lddy = (0, 0) if dy is None else (dy.data_ptr(), ld)
+    dh_at, lddh, y_at, ldy = 0, 0, 0, 0
+    if dh is not None:
+        dh_at, lddh = dh.data_ptr(), ld if dy is None else _ld(dh, "dh", like.dtype, gpu, rows, cols)
+        y_at, ldy = y.data_ptr(), _ld(y, "y", like.dtype, gpu, rows, cols)
 
     def matrix(t, name, wanted):
-        if not wanted:
-            if t is not None:
-                raise ValueError("%s: there is nothing to differentiate" % name)
-            return None, 0, 0
-        if t is None:
-            t = torch.empty(shape, dtype=like, device=device)
-        return t, t.data_ptr(), _ld(t, name, like, shape)
+        if wanted:
+            return _result(t, like, name, gpu, rows, cols)
+        if t is not None:
+            raise ValueError("%s: there is nothing to differentiate" % name)
+        return None, 0, 0
 
     dx, dx_at, lddx = matrix(dx, "dx", True)
     db, db_at, lddb = matrix(db, "db", b is not None)
@@ -325,17 +325,15 @@ def residual_grad(dy, dh, y, b, row_begin=None, index=None, norm="rms", post=Non
         if p is not None and grads[i] is None:
             if grad_index is not None:
                 raise ValueError("grad_index without %s" % name)
-            grads[i] = torch.empty((G, cols), dtype=torch.float32, device=device)
-        at, step, M = _vector(grads[i], name, cols, device, M)
+            grads[i] = like.new_empty((G, cols), dtype=torch.float32)
+        at, step, M = _vector(grads[i], name, cols, gpu, M)
         packed += [at, step]
     idx = None if M is None else _index(grad_index, G, M, "dpost, dpre, dgate")
-    _on(first)
-    out = _GRADS(0 if dy is None else dy.data_ptr(), lddy, 0 if dh is None else dh.data_ptr(), lddh, 0 if dh is None else y.data_ptr(), ldy,
-                 dx_at, lddx, db_at, lddb, dz_at, lddz, *packed, _address(idx))
+    out = _GRADS(dy_at, lddy, dh_at, lddh, y_at, ldy, dx_at, lddx, db_at, lddb, dz_at, lddz, *packed, _address(idx))
     lib = load()
-    need = lib.hop_residual_grad_scratch_bytes(a, out)
-    s = _scratch(need, device)
-    hop._check(lib.hop_residual_grad(a, out, s.data_ptr() if need else None, need, _stream(first)), "hop_residual_grad")
+    need = lib.hop_residual_grad_scratch_bytes(args, out)
+    s = _scratch(need, like)
+    hop._check(lib.hop_residual_grad(args, out, s.data_ptr() if need else None, need, _raw_stream(gpu)), "hop_residual_grad")
     del keep
     return ResidualGrads(dx, db, *grads, dlogits)
 
