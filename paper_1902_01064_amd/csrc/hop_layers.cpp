@@ -11,7 +11,7 @@
 namespace {
 
 constexpr uint64_t STREAM_DROPOUT = 8;         // beside hoprng's streams
-constexpr int64_t kMostRows = 0x7FFFFFFF - 65536;
+constexpr int64_t kMostRows = (1 << 30) - 65536;
 constexpr int64_t kMostCols = 1 << 21;         // a grid has room for 65535 tiles
 
 int hip_fail(hipError_t e, const char* what) {
@@ -74,6 +74,7 @@ HopProductTask product_task(const hop_product_args* a) {
     t.x = a->x; t.w = a->w; t.y = a->y;
     t.ldx = a->ldx; t.ldw = a->ldw; t.w_stride = a->w_stride; t.ldy = a->ldy;
     t.in = (int32_t)a->in; t.out = (int32_t)a->out; t.indexed = a->w_index != nullptr;
+    t.partial = nullptr;
     return t;
 }
 
@@ -83,6 +84,16 @@ bool product_grad_ok(const hop_product_grad_args* a) {
     return matrix_ok(a->dw, a->lddw, a->in, 4) && vectors_ok(nullptr, a->dw_stride) && index_ok(a->dw_index, a->groups.G) &&
            distinct(a->dw_index, a->groups.G) &&
            (a->groups.rows == 0 || (matrix_ok(a->dy, a->lddy, a->out, e) && matrix_ok(a->x, a->ldx, a->in, e)));
+}
+
+HopProductGradTask product_grad_task(const hop_product_grad_args* a) {
+    HopProductGradTask t;
+    t.rows = rows_of(a->groups);
+    t.dy = a->dy; t.x = a->x; t.dw = a->dw;
+    t.lddy = a->lddy; t.ldx = a->ldx; t.lddw = a->lddw; t.dw_stride = a->dw_stride;
+    t.in = (int32_t)a->in; t.out = (int32_t)a->out; t.indexed = a->dw_index != nullptr;
+    t.partial = nullptr;
+    return t;
 }
 
 bool residual_ok(const hop_residual_args* a) {
@@ -142,36 +153,45 @@ bool grads_ok(const hop_residual_args* a, const hop_residual_grads* g) {
 extern "C" {
 
 size_t hop_product_scratch_bytes(const hop_product_args* a) {
-    (void)a;
-    return 0;
+    if (!product_ok(a) || a->groups.rows == 0) return 0;
+    const HopProductPlan p = hopl_product_plan(product_task(a), a->groups.dtype, a->transposed != 0);
+    return p.parts > 1 ? (size_t)p.parts * (size_t)a->groups.rows * (size_t)a->out * 4 : 0;
 }
 
 int hop_product(const hop_product_args* a, void* scratch, size_t scratch_bytes, void* stream) {
-    (void)scratch, (void)scratch_bytes;
     if (!product_ok(a)) return HOP_ERR_INVALID_ARG;
     if (a->groups.rows == 0) return HOP_OK;
+    HopProductTask t = product_task(a);
+    const HopProductPlan p = hopl_product_plan(t, a->groups.dtype, a->transposed != 0);
+    if (p.parts > 1) {
+        if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
+        if (scratch_bytes < (size_t)p.parts * (size_t)t.rows.rows * (size_t)t.out * 4) return HOP_ERR_ARENA_TOO_SMALL;
+        t.partial = (float*)scratch;
+    }
     HopIndex index;
     hop_index_fill(&index, a->w_index, a->groups.G);
-    const int rc = hopl_product(product_task(a), a->groups.dtype, a->transposed != 0, index, stream);
+    const int rc = hopl_product(t, p, a->groups.dtype, a->transposed != 0, index, stream);
     return rc ? hip_fail((hipError_t)rc, "product launch") : HOP_OK;
 }
 
 size_t hop_product_grad_scratch_bytes(const hop_product_grad_args* a) {
-    (void)a;
-    return 0;
+    if (!product_grad_ok(a)) return 0;
+    const HopProductPlan p = hopl_product_grad_plan(product_grad_task(a), a->groups.dtype);
+    return p.parts > 1 ? (size_t)p.parts * (size_t)a->groups.G * (size_t)a->out * (size_t)a->in * 4 : 0;
 }
 
 int hop_product_grad(const hop_product_grad_args* a, void* scratch, size_t scratch_bytes, void* stream) {
-    (void)scratch, (void)scratch_bytes;
     if (!product_grad_ok(a)) return HOP_ERR_INVALID_ARG;
-    HopProductGradTask t;
-    t.rows = rows_of(a->groups);
-    t.dy = a->dy; t.x = a->x; t.dw = a->dw;
-    t.lddy = a->lddy; t.ldx = a->ldx; t.lddw = a->lddw; t.dw_stride = a->dw_stride;
-    t.in = (int32_t)a->in; t.out = (int32_t)a->out; t.indexed = a->dw_index != nullptr;
+    HopProductGradTask t = product_grad_task(a);
+    const HopProductPlan p = hopl_product_grad_plan(t, a->groups.dtype);
+    if (p.parts > 1) {
+        if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
+        if (scratch_bytes < (size_t)p.parts * (size_t)t.rows.G * (size_t)t.out * (size_t)t.in * 4) return HOP_ERR_ARENA_TOO_SMALL;
+        t.partial = (float*)scratch;
+    }
     HopIndex index;
     hop_index_fill(&index, a->dw_index, a->groups.G);
-    const int rc = hopl_product_grad(t, a->groups.dtype, index, stream);
+    const int rc = hopl_product_grad(t, p, a->groups.dtype, index, stream);
     return rc ? hip_fail((hipError_t)rc, "product gradient launch") : HOP_OK;
 }
 

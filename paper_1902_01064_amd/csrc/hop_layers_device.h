@@ -124,6 +124,74 @@ __device__ __forceinline__ int count_pieces(const HopRows& rows, int shift) {
     return __builtin_amdgcn_readfirstlane(n);
 }
 
+// The same with the shorter pieces at the groups' ends spread evenly between the whole ones: the short ones are bound by reading weights, the
+// whole ones by arithmetic, and they are to run side by side.  count_whole gives both numbers; find_whole takes a piece by its place.
+struct WholePieces {
+    int whole, rest;
+};
+__device__ __forceinline__ WholePieces count_whole(const HopRows& rows, int shift) {
+    const int part = (1 << shift) - 1;
+    if (!rows.begin) return {rows.rows >> shift, (rows.rows & part) != 0};
+    const HOPL_GLOBAL int32_t* table = (const HOPL_GLOBAL int32_t*)rows.begin;
+    int whole = 0, rest = 0;
+    for (int g = threadIdx.x & 63; g < rows.G; g += 64) {
+        const int b = clamp_int(table[g], 0, rows.rows), n = clamp_int(table[g + 1], b, rows.rows) - b;
+        whole += n >> shift;
+        rest += (n & part) != 0;
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        whole += __shfl_xor(whole, o);
+        rest += __shfl_xor(rest, o);
+    }
+    return {__builtin_amdgcn_readfirstlane(whole), __builtin_amdgcn_readfirstlane(rest)};
+}
+__device__ __forceinline__ bool find_whole(const HopRows& rows, int shift, WholePieces all, int piece, int* g, int* r0, int* r1) {
+    const int step = 1 << shift;
+    if (!rows.begin) {
+        *g = 0;
+        *r0 = piece << shift;
+        *r1 = min(*r0 + step, rows.rows);
+        return *r0 < *r1;
+    }
+    const int64_t total = (int64_t)all.whole + all.rest;
+    const int rests = (int)(((int64_t)piece * all.rest) / total), then = (int)(((int64_t)(piece + 1) * all.rest) / total);
+    const bool last = then > rests;
+    piece = last ? rests : piece - rests;
+    const int lane = threadIdx.x & 63;
+    const HOPL_GLOBAL int32_t* table = (const HOPL_GLOBAL int32_t*)rows.begin;
+    int seen = 0;
+    for (int base = 0; base < rows.G; base += 64) {
+        const int mine = base + lane;
+        int b = 0, e = 0;
+        if (mine < rows.G) {
+            b = clamp_int(table[mine], 0, rows.rows);
+            e = clamp_int(table[mine + 1], b, rows.rows);
+        }
+        const int own = last ? ((e - b) & (step - 1)) != 0 : (e - b) >> shift;
+        int scan = own;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int before = __shfl_up(scan, o);
+            if (lane >= o) scan += before;
+        }
+        const uint64_t behind = __ballot(seen + scan > piece);
+        if (behind) {
+            const int l = __builtin_ctzll(behind);
+            const int gb = __builtin_amdgcn_readlane(b, l), ge = __builtin_amdgcn_readlane(e, l);
+            const int first = seen + __builtin_amdgcn_readlane(scan, l) - __builtin_amdgcn_readlane(own, l);
+            const int64_t at = last ? ge - ((ge - gb) & (step - 1)) : gb + ((int64_t)(piece - first) << shift);
+            if (at < gb || at >= ge) return false;        // only where a broken table made the sums overflow
+            *g = base + l;
+            *r0 = (int)at;
+            *r1 = ge - at < step ? ge : (int)at + step;
+            return true;
+        }
+        seen += __builtin_amdgcn_readlane(scan, 63);
+    }
+    return false;
+}
+
 // The rows of group g.
 __device__ __forceinline__ void group_rows(const HopRows& rows, int g, int* b, int* e) {
     if (!rows.begin) {

@@ -24,6 +24,7 @@ struct HopProductTask {            // y = x w^T or x w, row by row with the grou
     const void *x, *w;
     void* y;
     int64_t ldx, ldw, w_stride, ldy;
+    float* partial;                // [parts][rows][out] where the contraction is cut in parts
     int32_t in, out, indexed;
 };
 
@@ -32,7 +33,15 @@ struct HopProductGradTask {        // dw = dy^T x over the group's rows
     const void *dy, *x;
     float* dw;
     int64_t lddy, ldx, lddw, dw_stride;
+    float* partial;                // [parts][G][out][in] where the rows are cut in parts
     int32_t in, out, indexed;
+};
+
+// How a product is computed: by tiles fed through registers, of any alignment; by tiles fed to LDS by the memory unit; by tiles of few
+// rows whose weights go straight to registers.  Decided from sizes, types and alignment alone.
+enum { HOPL_ANY = 0, HOPL_STAGED = 1, HOPL_FEW = 2 };
+struct HopProductPlan {
+    int kind, parts, tile;
 };
 
 struct HopMask {                   // of a dropout: key, first row, threshold and factor
@@ -63,8 +72,10 @@ struct HopResidualTask {
 };
 
 // Kernel launchers; each returns a hipError_t as int.
-int hopl_product(const HopProductTask& t, int dtype, int transposed, const HopIndex& index, void* stream);
-int hopl_product_grad(const HopProductGradTask& t, int dtype, const HopIndex& index, void* stream);
+HopProductPlan hopl_product_plan(const HopProductTask& t, int dtype, int transposed);
+HopProductPlan hopl_product_grad_plan(const HopProductGradTask& t, int dtype);
+int hopl_product(const HopProductTask& t, const HopProductPlan& p, int dtype, int transposed, const HopIndex& index, void* stream);
+int hopl_product_grad(const HopProductGradTask& t, const HopProductPlan& p, int dtype, const HopIndex& index, void* stream);
 int hopl_dropout(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int64_t cols, const HopMask& m, void* stream);
 int hopl_residual(HopResidualTask t, int dtype, const HopIndex& index, void* stream);
 int hopl_residual_grad(HopResidualTask t, int dtype, const HopIndex& index, const HopIndex& dindex, void* stream);
