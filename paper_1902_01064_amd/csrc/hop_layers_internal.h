@@ -39,7 +39,7 @@ struct HopProductGradTask {        // dw = dy^T x over the group's rows
 
 // How a product is computed: by tiles fed through registers, of any alignment; by tiles fed to LDS by the memory unit; by tiles of few
 // rows whose weights go straight to registers.  Decided from sizes, types and alignment alone.
-enum { HOPL_ANY = 0, HOPL_STAGED = 1, HOPL_FEW = 2 };
+enum { HOPL_ANY = 0, HOPL_FED = 1, HOPL_FEW = 2 };
 struct HopProductPlan {
     int kind, parts, tile;
 };

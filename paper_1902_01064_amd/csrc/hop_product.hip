@@ -9,119 +9,7 @@ using namespace hopl;
 
 namespace {
 
-constexpr int kTile = 64;               // rows and columns of a workgroup's tile
-constexpr int kStep = 32;               // of the contraction per turn
-constexpr int kThreads = 256;
-
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-template <typename T>
-struct Raw;                             // eight elements as they are
-template <>
-struct Raw<bf16> { typedef bf16x8 type; typedef bf16x8_any any; };
-template <>
-struct Raw<float> { typedef f32x8 type; typedef f32x8_any any; };
-
-template <typename T>
-__device__ __forceinline__ typename Raw<T>::type raw8(const T* p, int n) {
-    if (n >= 8) return *(const HOPL_GLOBAL typename Raw<T>::any*)p;
-    typename Raw<T>::type v = (T)0.f;
-#pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (i < n) v[i] = ((const HOPL_GLOBAL T*)p)[i];
-    return v;
-}
-
-// One operand of a tile, kTile lines (rows or columns of the result) by kStep of the contraction.  ALONG: the contraction is
-// contiguous in memory (element (line, k) at p[line * ld + k]), else the lines are (p[k * ld + line]); it lies in LDS as in memory.
-// What lies outside the operand is zero in LDS: a neighbouring group's rows never meet this group's sums, whatever they hold.
-template <typename T, bool ALONG>
-struct Operand {
-    static constexpr int kPad = 16 / sizeof(T);
-    static constexpr int kLd = (ALONG ? kStep : kTile) + kPad;
-    static constexpr int kElems = (ALONG ? kTile : kStep) * kLd;
-    typename Raw<T>::type part;
-
-    __device__ __forceinline__ void load(const T* p, int64_t ld, int lines, int k0, int K) {
-        const int a = ALONG ? threadIdx.x >> 2 : threadIdx.x >> 3;
-        const int b = ALONG ? (threadIdx.x & 3) * 8 : (threadIdx.x & 7) * 8;
-        const int have_a = ALONG ? lines : K - k0, have_b = ALONG ? K - k0 : lines;
-        part = (T)0.f;
-        if (a < have_a && b < have_b)
-            part = raw8(ALONG ? p + a * ld + (k0 + b) : p + (int64_t)(k0 + a) * ld + b, have_b - b);
-    }
-    __device__ __forceinline__ void put(T* s) const {
-        const int a = ALONG ? threadIdx.x >> 2 : threadIdx.x >> 3;
-        const int b = ALONG ? (threadIdx.x & 3) * 8 : (threadIdx.x & 7) * 8;
-        *(typename Raw<T>::type*)(s + a * kLd + b) = part;
-    }
-};
-
-// acc[i][j]: rows p0 + 16 j + lane % 16, columns q0 + 16 i + 4 (lane / 16) ..: the columns' operand is the first of the matrix
-// instruction, so that a lane holds four consecutive columns of one row.
-template <bool PA, bool QA>
-__device__ __forceinline__ void multiply(const bf16* sp, const bf16* sq, int p0, int q0, f32x4 (&acc)[2][2]) {
-    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
-    bf16x8 p[2], q[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const bool along = which ? QA : PA;
-            const bf16* s = which ? sq : sp;
-            const int at = (which ? q0 : p0) + 16 * i;
-            bf16x8 v;
-            if (along) {
-                v = *(const bf16x8*)(s + (at + l16) * Operand<bf16, true>::kLd + quad * 8);
-            } else {
-                // the transposing read: 16 lanes hold four lines of 16 elements, lane l gets column l of them
-                const bf16* a = s + (quad * 8 + (l16 >> 2)) * Operand<bf16, false>::kLd + at + (l16 & 3) * 4;
-                union { s16x4 half[2]; bf16x8 all; } u;
-                u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)a);
-                u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(a + 4 * Operand<bf16, false>::kLd));
-                v = u.all;
-            }
-            (which ? q : p)[i] = v;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[i], p[j], acc[i][j], 0, 0, 0);
-}
-
-// fp32: 16 x 16 x 4 instructions; the contraction's order is the operands' own affair, so a lane takes four consecutive k.
-template <bool PA, bool QA>
-__device__ __forceinline__ void multiply(const float* sp, const float* sq, int p0, int q0, f32x4 (&acc)[2][2]) {
-    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
-#pragma unroll
-    for (int k = 0; k < kStep; k += 16) {
-        f32x4 p[2], q[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                const bool along = which ? QA : PA;
-                const float* s = which ? sq : sp;
-                const int at = (which ? q0 : p0) + 16 * i + l16, k4 = k + quad * 4;
-                f32x4 v;
-                if (along) {
-                    v = *(const f32x4*)(s + at * Operand<float, true>::kLd + k4);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = s[(k4 + e) * Operand<float, false>::kLd + at];
-                }
-                (which ? q : p)[i] = v;
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(q[i][e], p[j][e], acc[i][j], 0, 0, 0);
-    }
-}
 
 __device__ __forceinline__ void store4(float* p, int n, f32x4 v) {
     if (n >= 4) {
@@ -141,41 +29,6 @@ __device__ __forceinline__ void store4(bf16* p, int n, f32x4 v) {
 #pragma unroll
     for (int i = 0; i < 3; ++i)
         if (i < n) ((HOPL_GLOBAL bf16*)p)[i] = r[i];
-}
-
-// c[p][q] = sum over k of P(p, k) Q(q, k), one tile of it: `np` rows and `nq` columns exist from here on.
-template <typename T, typename OUT, bool PA, bool QA>
-__device__ __forceinline__ void tile_product(const T* p, int64_t ldp, int np, const T* q, int64_t ldq, int nq, int K, OUT* c, int64_t ldc) {
-    typedef Operand<T, PA> P;
-    typedef Operand<T, QA> Q;
-    __shared__ __attribute__((aligned(16))) T sp[P::kElems], sq[Q::kElems];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int p0 = (wave & 1) * 32, q0 = (wave >> 1) * 32;
-    f32x4 acc[2][2] = {};
-    P rp;
-    Q rq;
-    if (K > 0) {
-        rp.load(p, ldp, np, 0, K);
-        rq.load(q, ldq, nq, 0, K);
-    }
-    for (int k = 0; k < K; k += kStep) {
-        __syncthreads();
-        rp.put(sp);
-        rq.put(sq);
-        __syncthreads();
-        if (K - k > kStep) {
-            rp.load(p, ldp, np, k + kStep, K);
-            rq.load(q, ldq, nq, k + kStep, K);
-        }
-        multiply<PA, QA>(sp, sq, p0, q0, acc);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int row = p0 + 16 * j + (lane & 15), col = q0 + 16 * i + 4 * (lane >> 4);
-            if (row < np && col < nq) store4(c + row * ldc + col, nq - col, acc[i][j]);
-        }
 }
 
 // ---- staged tiles -------------------------------------------------------------------
@@ -232,6 +85,64 @@ struct Feed {
             uint32_t o = off[i];
             if (ALONG && first[i] >= left) o = kOutside;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(stage + (i * NT + wave * 64) * 16), 16, o, 0, 0, 0);
+        }
+    }
+};
+
+// The same for operands of any alignment, through registers: 128-bit loads at an element's address, chunks cut where the operand ends.
+template <typename T, bool ALONG, int LINES, int NT>
+struct RegisterFeed {
+    static constexpr int kChunk = 16 / sizeof(T), kK = kStepBytes / sizeof(T), kPerLine = ALONG ? 8 : LINES / kChunk, kLoads = LINES * 8 / NT;
+    static constexpr int kBytes = LINES * kStepBytes;
+    typedef T chunk __attribute__((ext_vector_type(kChunk)));
+    typedef chunk chunk_any __attribute__((aligned(sizeof(T))));
+    const T* base;
+    int64_t ld;
+    int lines, K;
+    chunk part[kLoads];
+
+    __device__ __forceinline__ void start(const T* p, int64_t ld_, int lines_, int K_) {
+        base = p;
+        ld = ld_;
+        lines = lines_ < LINES ? lines_ : LINES;
+        K = K_;
+    }
+    // Chunks that begin inside the operand are loaded whole wherever that stays in front of its last element.  What they hold beyond the
+    // contraction's end is set to zero on the way to LDS (not here: the loads are to be on their way through a turn); beyond the last line
+    // they fill lines whose results nobody stores.
+    __device__ __forceinline__ void fetch(int k) {
+        const int64_t end = ALONG ? (lines - 1) * ld + K : (K - 1) * ld + lines;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int j = i * NT + threadIdx.x, l = j / kPerLine, c = j % kPerLine * kChunk;
+            const int n = ALONG ? (l < lines ? K - k - c : 0) : (k + l < K ? lines - c : 0);
+            const int64_t off = ALONG ? l * ld + (k + c) : (int64_t)(k + l) * ld + c;
+            part[i] = (T)0.f;
+            if (n <= 0) continue;
+            const HOPL_GLOBAL T* p = (const HOPL_GLOBAL T*)(base + off);
+            if (off + kChunk <= end) {
+                part[i] = *(const HOPL_GLOBAL chunk_any*)p;
+            } else {
+#pragma unroll
+                for (int e = 0; e < kChunk; ++e)
+                    if (e < n) part[i][e] = p[e];
+            }
+        }
+    }
+    __device__ __forceinline__ void put(char* stage, int k) {
+        if (ALONG && K - k < kK) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int n = K - k - (i * NT + (int)threadIdx.x) % kPerLine * kChunk;
+#pragma unroll
+                for (int e = 0; e < kChunk; ++e)
+                    if (e >= n) part[i][e] = (T)0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int j = i * NT + threadIdx.x, l = j / kPerLine, c = (j % kPerLine) ^ Feed<T, ALONG, LINES, NT>::swizzle(l);
+            *(chunk*)(stage + (l * kPerLine + c) * 16) = part[i];
         }
     }
 };
@@ -298,7 +209,7 @@ __device__ __forceinline__ void arrive() {
     asm volatile("" ::: "memory");
 }
 
-template <typename T, typename OUT, bool PA, bool QA, int BM, int BN, int WM, int WN>
+template <typename T, typename OUT, bool PA, bool QA, bool FED, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void staged_product(const T* p, int64_t ldp, int np, const T* q, int64_t ldq, int nq, int K, OUT* c, int64_t ldc) {
     typedef Unit<T> U;
     constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, FM = TM / U::kLines, FN = TN / U::kLines;
@@ -306,8 +217,8 @@ __device__ __forceinline__ void staged_product(const T* p, int64_t ldp, int np, 
     // Which operand comes first decides what a lane holds of the result: four consecutive columns of a row, or four rows of a column.
     // For results in 32 bits of a 32-line unit the latter: 32 lanes store 128 consecutive bytes of a row.
     constexpr bool kSwap = sizeof(OUT) == 4 && U::kLines == 32;
-    typedef Feed<T, PA, BM, NT> P;
-    typedef Feed<T, QA, BN, NT> Q;
+    typedef std::conditional_t<FED, Feed<T, PA, BM, NT>, RegisterFeed<T, PA, BM, NT>> P;
+    typedef std::conditional_t<FED, Feed<T, QA, BN, NT>, RegisterFeed<T, QA, BN, NT>> Q;
     // arrays of their own, so that the compiler knows that reads of one stage need not wait for loads into the other
     __shared__ __attribute__((aligned(16))) char sp0[P::kBytes], sq0[Q::kBytes], sp1[P::kBytes], sq1[Q::kBytes];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -322,13 +233,28 @@ __device__ __forceinline__ void staged_product(const T* p, int64_t ldp, int np, 
     // Tiles of few rows are bound by reading the other operand, whose lines are a power of two apart as a rule: workgroups that walk along
     // them side by side would all ask the same memory channels.  So they begin at different places and go round.
     const int steps = (K + kK - 1) / kK, rotate = np <= kNext && steps ? (int)(blockIdx.x / 8 % steps) : 0;
+    auto begins = [&](int step) { return (step + rotate < steps ? step + rotate : step + rotate - steps) * kK; };
     auto issue = [&](char* sp, char* sq, int step) {
-        step += rotate;
-        if (step >= steps) step -= steps;
-        fp.issue(sp, step * kK);
-        fq.issue(sq, step * kK);
+        const int k = begins(step);
+        if constexpr (FED) {
+            fp.issue(sp, k);
+            fq.issue(sq, k);
+        } else {
+            fp.fetch(k);
+            fq.fetch(k);
+        }
     };
-    if (steps) issue(sp0, sq0, 0);
+    auto put = [&](char* sp, char* sq, int step) {            // behind the turn that the loads ran beside
+        if constexpr (!FED) {
+            const int k = begins(step);
+            fp.put(sp, k);
+            fq.put(sq, k);
+        }
+    };
+    if (steps) {
+        issue(sp0, sq0, 0);
+        put(sp0, sq0, 0);
+    }
     auto run = [&](auto live) {
         constexpr int kLive = decltype(live)::value;
         auto turn = [&](const char* sp, const char* sq) {
@@ -357,9 +283,11 @@ __device__ __forceinline__ void staged_product(const T* p, int64_t ldp, int np, 
             arrive();
             issue(sp1, sq1, step + 1);
             turn(sp0, sq0);
+            put(sp1, sq1, step + 1);
             arrive();
             if (step + 2 < steps) issue(sp0, sq0, step + 2);
             turn(sp1, sq1);
+            if (step + 2 < steps) put(sp0, sq0, step + 2);
         }
         if (step < steps) {
             arrive();
@@ -407,7 +335,9 @@ __device__ __forceinline__ void staged_product(const T* p, int64_t ldp, int np, 
 constexpr int kBand = 4, kRun = 32;
 __device__ __forceinline__ bool place_tile(int b, int pieces, int columns, int* piece, int* column) {
     pieces = min(pieces, (int)gridDim.x / columns);         // what a proper row table has at most
-    const int total = pieces * columns, run = min(max((total + 7) / 8, 1), kRun), turn = b / 8;
+    const int total = pieces * columns, rounds = (total + 8 * kRun - 1) / (8 * kRun);
+    if (!total) return false;
+    const int run = (total + 8 * rounds - 1) / (8 * rounds), turn = b / 8;      // as many runs for every XCD
     const int at = (turn / run * 8 + b % 8) * run + turn % run;
     if (at >= total) return false;
     const int band = at / (kBand * columns), within = at - band * kBand * columns;
@@ -418,7 +348,7 @@ __device__ __forceinline__ bool place_tile(int b, int pieces, int columns, int* 
 }
 
 // PART: the contraction is cut in gridDim.y parts, whose sums go to partial[part][row][column] in 32 bits.
-template <typename T, bool TRANSPOSED, bool PART, int BM, int BN, int WM, int WN>
+template <typename T, bool TRANSPOSED, bool PART, bool FED, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM* WN * 64) void product_staged_kernel(HopProductTask t, int columns, HopIndex index) {
     constexpr int shift = __builtin_ctz(BM), kK = kStepBytes / sizeof(T);
     int piece, column, g, r0, r1;
@@ -434,16 +364,16 @@ __global__ __launch_bounds__(WM* WN * 64) void product_staged_kernel(HopProductT
     const T* w = (const T*)t.w + at * t.w_stride + (TRANSPOSED ? n0 : n0 * t.ldw);
     if constexpr (PART) {
         const int each = ((t.in + gridDim.y - 1) / gridDim.y + kK - 1) / kK * kK, k0 = min((int)blockIdx.y * each, t.in);
-        staged_product<T, float, true, !TRANSPOSED, BM, BN, WM, WN>(x + k0, t.ldx, r1 - r0, w + (TRANSPOSED ? k0 * t.ldw : k0), t.ldw, (int)(t.out - n0),
+        staged_product<T, float, true, !TRANSPOSED, FED, BM, BN, WM, WN>(x + k0, t.ldx, r1 - r0, w + (TRANSPOSED ? k0 * t.ldw : k0), t.ldw, (int)(t.out - n0),
                                                                     min(each, t.in - k0),
                                                                     t.partial + ((int64_t)blockIdx.y * t.rows.rows + r0) * t.out + n0, t.out);
     } else {
-        staged_product<T, T, true, !TRANSPOSED, BM, BN, WM, WN>(x, t.ldx, r1 - r0, w, t.ldw, (int)(t.out - n0), t.in, (T*)t.y + r0 * t.ldy + n0, t.ldy);
+        staged_product<T, T, true, !TRANSPOSED, FED, BM, BN, WM, WN>(x, t.ldx, r1 - r0, w, t.ldw, (int)(t.out - n0), t.in, (T*)t.y + r0 * t.ldy + n0, t.ldy);
     }
 }
 
 // PART: the group's rows are cut in gridDim.y parts, whose sums go to partial[part][g][out][in].
-template <typename T, bool PART, int BM, int BN, int WM, int WN>
+template <typename T, bool PART, bool FED, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM* WN * 64) void product_grad_staged_kernel(HopProductGradTask t, int tiles_out, int tiles_in, HopIndex index) {
     constexpr int kK = kStepBytes / sizeof(T);
     // Groups differ in length, so every group's tiles are dealt to all XCDs, a run of them to each (operands' tiles are shared in its L2).
@@ -463,7 +393,7 @@ __global__ __launch_bounds__(WM* WN * 64) void product_grad_staged_kernel(HopPro
         to = t.partial + (((int64_t)blockIdx.y * t.rows.G + g) * t.out + o0) * t.in + i0;
         ld = t.in;
     }
-    staged_product<T, float, false, false, BM, BN, WM, WN>((const T*)t.dy + b * t.lddy + o0, t.lddy, (int)(t.out - o0), (const T*)t.x + b * t.ldx + i0,
+    staged_product<T, float, false, false, FED, BM, BN, WM, WN>((const T*)t.dy + b * t.lddy + o0, t.lddy, (int)(t.out - o0), (const T*)t.x + b * t.ldx + i0,
                                                            t.ldx, (int)(t.in - i0), e - b, to, ld);
 }
 
@@ -551,28 +481,6 @@ __global__ __launch_bounds__(kFewWaves * 64) void product_few_kernel(HopProductT
     if (row < r1 - r0 && col < columns) store4((T*)t.y + (r0 + row) * t.ldy + n0 + col, columns - col, v);
 }
 
-template <typename T, bool TRANSPOSED>
-__global__ __launch_bounds__(kThreads) void product_kernel(HopProductTask t, HopIndex index) {
-    int g, r0, r1;
-    if (!find_piece(t.rows, 6, blockIdx.x, &g, &r0, &r1)) return;
-    const int64_t n0 = (int64_t)blockIdx.y * kTile;
-    const int at = t.indexed ? index.at[g] : g;
-    const T* w = (const T*)t.w + at * t.w_stride + (TRANSPOSED ? n0 : n0 * t.ldw);
-    tile_product<T, T, true, !TRANSPOSED>((const T*)t.x + r0 * t.ldx, t.ldx, r1 - r0, w, t.ldw, (int)(t.out - n0), t.in,
-                                          (T*)t.y + r0 * t.ldy + n0, t.ldy);
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void product_grad_kernel(HopProductGradTask t, HopIndex index) {
-    const int g = blockIdx.z;
-    int b, e;
-    group_rows(t.rows, g, &b, &e);
-    const int64_t o0 = (int64_t)blockIdx.y * kTile, i0 = (int64_t)blockIdx.x * kTile;
-    const int at = t.indexed ? index.at[g] : g;
-    tile_product<T, float, false, false>((const T*)t.dy + b * t.lddy + o0, t.lddy, (int)(t.out - o0), (const T*)t.x + b * t.ldx + i0, t.ldx,
-                                         (int)(t.in - i0), e - b, t.dw + at * t.dw_stride + o0 * t.lddw + i0, t.lddw);
-}
-
 // Whether an operand can be fed by 128-bit loads: addresses and distances are multiples of 16 bytes, `cols` (the contiguous direction) of
 // whole chunks, and a tile's offsets fit 31 bits.
 bool feedable(const void* p, int64_t ld, int64_t stride, int64_t cols, size_t elem) {
@@ -583,21 +491,28 @@ bool feedable(const void* p, int64_t ld, int64_t stride, int64_t cols, size_t el
 // The most pieces of `step` rows that G groups can leave: each group with rows has at most step - 1 of them missing from its last.
 int64_t pieces_of(const HopRows& rows, int step) { return (rows.rows + (int64_t)(step - 1) * (rows.G < rows.rows ? rows.G : rows.rows)) / step; }
 // Workgroups that place_tile needs to see them all.
-int64_t tile_grid(int64_t tiles) { return tiles < 8 * kRun ? (tiles + 7) / 8 * 8 : (tiles + 8 * kRun - 1) / (8 * kRun) * (8 * kRun); }
+int64_t tile_grid(int64_t tiles) { return 8 * ((tiles + 7) / 8 + (tiles + 8 * kRun - 1) / (8 * kRun)); }
 
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, bool FED, int BM, int BN, int WM, int WN>
 void launch_staged(const HopProductTask& t, int transposed, int parts, const HopIndex& index, hipStream_t st) {
     const int64_t columns = (t.out + BN - 1) / BN, tiles = pieces_of(t.rows, BM) * columns;
     const dim3 grid((unsigned)tile_grid(tiles), (unsigned)parts), block(WM * WN * 64);
     if (parts > 1) {
-        if (transposed) product_staged_kernel<T, true, true, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
-        else product_staged_kernel<T, false, true, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
+        if (transposed) product_staged_kernel<T, true, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
+        else product_staged_kernel<T, false, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
         product_join_kernel<T><<<join_blocks(t.rows.rows, t.out), 256, 0, st>>>(t.partial, parts, t.rows.rows, t.out, (T*)t.y, t.ldy, 0, 0, 0, index);
     } else {
-        if (transposed) product_staged_kernel<T, true, false, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
-        else product_staged_kernel<T, false, false, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
+        if (transposed) product_staged_kernel<T, true, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
+        else product_staged_kernel<T, false, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
     }
 }
+template <typename T, bool FED>
+void launch_tile(const HopProductTask& t, int transposed, const HopProductPlan& p, const HopIndex& index, hipStream_t st) {
+    if (p.tile == 1) launch_staged<T, FED, 128, 128, 2, 2>(t, transposed, p.parts, index, st);
+    else if (p.tile == 2) launch_staged<T, FED, 64, 64, 2, 2>(t, transposed, p.parts, index, st);
+    else launch_staged<T, FED, 32, 128, 1, 4>(t, transposed, p.parts, index, st);
+}
+
 template <typename T>
 void launch_few(const HopProductTask& t, int tile, const HopIndex& index, hipStream_t st) {
     const dim3 grid((unsigned)((t.out + 15) / 16), (unsigned)pieces_of(t.rows, tile & 1 ? 32 : 16));
@@ -607,16 +522,16 @@ void launch_few(const HopProductTask& t, int tile, const HopIndex& index, hipStr
     else product_few_kernel<T, 2, 16><<<grid, 1024, 0, st>>>(t, index);
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, bool FED, int BM, int BN, int WM, int WN>
 void launch_grad_staged(const HopProductGradTask& t, int parts, const HopIndex& index, hipStream_t st) {
     const int64_t out = (t.out + BM - 1) / BM, in = (t.in + BN - 1) / BN;
     const dim3 grid((unsigned)(t.rows.G * ((out * in + 7) / 8 * 8)), (unsigned)parts);
     if (parts > 1) {
-        product_grad_staged_kernel<T, true, BM, BN, WM, WN><<<grid, WM * WN * 64, 0, st>>>(t, (int)out, (int)in, index);
+        product_grad_staged_kernel<T, true, FED, BM, BN, WM, WN><<<grid, WM * WN * 64, 0, st>>>(t, (int)out, (int)in, index);
         const int64_t rows = (int64_t)t.rows.G * t.out;
         product_join_kernel<float><<<join_blocks(rows, t.in), 256, 0, st>>>(t.partial, parts, rows, t.in, t.dw, t.lddw, t.out, t.dw_stride, t.indexed, index);
     } else {
-        product_grad_staged_kernel<T, false, BM, BN, WM, WN><<<grid, WM * WN * 64, 0, st>>>(t, (int)out, (int)in, index);
+        product_grad_staged_kernel<T, false, FED, BM, BN, WM, WN><<<grid, WM * WN * 64, 0, st>>>(t, (int)out, (int)in, index);
     }
 }
 
@@ -630,15 +545,15 @@ struct TileCost {
     double full, least, own;
     int beside;
 };
-constexpr TileCost kTilesBf16[3] = {{256, 256, 64, 1.75, 0.85, 0.0, 1}, {128, 128, 64, 0.49, 0.55, 0.0, 2}, {32, 128, 32, 0.32, 0.46, 0.0, 4}};
-constexpr TileCost kTilesF32[3] = {{128, 128, 32, 1.91, 0.75, 0.0, 2}, {64, 128, 32, 0.98, 0.72, 0.0, 3}, {32, 128, 16, 0.50, 0.60, 0.0, 4}};
+constexpr TileCost kTilesBf16[4] = {{256, 256, 64, 1.75, 0.85, 0.0, 1}, {128, 128, 64, 0.49, 0.55, 0.0, 2}, {64, 64, 64, 0.24, 0.45, 0.0, 5}, {32, 128, 32, 0.28, 0.46, 0.0, 4}};
+constexpr TileCost kTilesF32[4] = {{0, 0, 0, 0, 0, 0, 0}, {128, 128, 32, 1.91, 0.75, 0.0, 2}, {64, 64, 32, 0.49, 0.62, 0.0, 5}, {32, 128, 16, 0.50, 0.60, 0.0, 4}};
 constexpr TileCost kGradTilesBf16[3] = {{256, 256, 64, 1.75, 1.1, 0.0, 1}, {128, 128, 64, 0.60, 0.67, 0.5, 2}, {64, 64, 64, 0.35, 0.45, 0.3, 4}};
 constexpr TileCost kGradTilesF32[2] = {{128, 128, 32, 1.93, 2.1, 0.0, 2}, {64, 64, 32, 0.48, 0.65, 0.2, 4}};
 constexpr double kCus = 256, kHbm = 5.2e6, kJoin = 6e6, kLaunch = 4;       // bytes a us; us
 
 // Steps of `units` workgroups; `fill`: the part of a tile that is not padding.
 double steps_time(const TileCost& c, double units, double steps, double fill) {
-    const double each = std::max(1.0, units / kCus), one = std::max(c.least, c.beside == 1 ? c.full * fill : 1.1 * c.full * fill);
+    const double each = std::max(1.0, std::ceil(units / kCus)), one = std::max(c.least, c.beside == 1 ? c.full * fill : 1.1 * c.full * fill);
     return steps * std::max(std::ceil(each / c.beside) * one, each * c.full * fill) + each * c.own;
 }
 
@@ -648,17 +563,18 @@ double together(double a, double b) { return std::max(a, b) + 0.1 * std::min(a, 
 }  // namespace
 
 HopProductPlan hopl_product_plan(const HopProductTask& t, int dtype, int transposed) {
-    HopProductPlan best = {HOPL_ANY, 1, 0};
+    HopProductPlan best = {HOPL_ANY, 1, 1};
     const size_t e = dtype == HOP_BF16 ? 2 : 4;
-    if (!feedable(t.x, t.ldx, 0, t.in, e) || !feedable(t.w, t.ldw, t.w_stride, transposed ? t.out : t.in, e)) return best;
+    const bool fed = feedable(t.x, t.ldx, 0, t.in, e) && feedable(t.w, t.ldw, t.w_stride, transposed ? t.out : t.in, e);
     const double T = t.rows.rows, G = std::min((double)t.rows.G, T), R = T / G, in = t.in, out = t.out;
     const double bytes = e * (G * in * out + T * in + T * out) / kHbm;
     double least = 1e300;
     auto consider = [&](double us, HopProductPlan p) {
         if (us < least) least = us, best = p;
     };
-    for (int i = 0; i < 3; ++i) {
-        const TileCost& c = dtype == HOP_BF16 ? kTilesBf16[i] : kTilesF32[i];
+    for (int i = fed && dtype == HOP_BF16 ? 0 : 1; i < 4; ++i) {
+        TileCost c = dtype == HOP_BF16 ? kTilesBf16[i] : kTilesF32[i];
+        if (dtype == HOP_F32 && transposed && i == 2) c.full *= 1.15;          // its reads of single words from LDS (4096^3: 1157 us, 1000 the other way)
         if (pieces_of(t.rows, c.bm) * ((t.out + c.bn - 1) / c.bn) > 1 << 22) continue;
         const double per = R <= c.bm / 2 ? 1 : R / c.bm + 0.5, fill = std::min(1.0, (R + c.grain / 2) / (per * c.bm));
         const double units = G * per * std::ceil(out / c.bn), steps = std::ceil(in * e / kStepBytes);
@@ -666,13 +582,13 @@ HopProductPlan hopl_product_plan(const HopProductTask& t, int dtype, int transpo
             if (parts > 1 && (steps < 2 * parts || units * parts > 4 * kCus)) break;
             double us = kLaunch + together(bytes, steps_time(c, units * parts, std::ceil(steps / parts), fill));
             if (parts > 1) us += 3 + parts * T * out * 8 / kJoin;
-            consider(us, {HOPL_STAGED, parts, i});
+            consider(us, {fed ? HOPL_FED : HOPL_ANY, parts, i});
         }
     }
     // Few rows: a turn of all wavefronts takes 1.25 us when nothing else is in its way; with 32 rows the weights come at 3 TB/s (64 rows of
     // 4096 x 4096 in bf16 26 us), with 16 at 5 (33 us).  Sixteen wavefronts where there are too few workgroups for four of them each (1 row, 8192 x 1024:
     // 14.2 -> 12.7 us; 8 rows over 8 groups of 1024 x 1024 6.6 -> 9.6).
-    if (!transposed && R <= 64 && T * in * out < 1e12) {
+    if (fed && !transposed && R <= 64 && T * in * out < 1e12) {
         for (int wide = 0; wide < 2; ++wide) {
             const double pieces = G * std::max(1.0, R <= (wide ? 32 : 16) ? 1.0 : R / (wide ? 32 : 16) + 0.5), units = pieces * std::ceil(out / 16);
             const double turns = std::ceil(in * e / 2048.0);
@@ -685,12 +601,12 @@ HopProductPlan hopl_product_plan(const HopProductTask& t, int dtype, int transpo
 }
 
 HopProductPlan hopl_product_grad_plan(const HopProductGradTask& t, int dtype) {
-    HopProductPlan best = {HOPL_ANY, 1, 0};
+    HopProductPlan best = {HOPL_ANY, 1, dtype == HOP_BF16 ? 1 : 0};
     const size_t e = dtype == HOP_BF16 ? 2 : 4;
-    if (!feedable(t.dy, t.lddy, 0, t.out, e) || !feedable(t.x, t.ldx, 0, t.in, e)) return best;
+    const bool fed = feedable(t.dy, t.lddy, 0, t.out, e) && feedable(t.x, t.ldx, 0, t.in, e);
     const double G = t.rows.G, R = std::max(1.0, t.rows.rows / G), written = G * t.in * t.out * 4.0;
     double least = 1e300;
-    for (int i = 0; i < (dtype == HOP_BF16 ? 3 : 2); ++i) {
+    for (int i = fed || dtype != HOP_BF16 ? 0 : 1; i < (dtype == HOP_BF16 ? 3 : 2); ++i) {
         const TileCost& c = dtype == HOP_BF16 ? kGradTilesBf16[i] : kGradTilesF32[i];
         const double units = G * std::ceil((double)t.out / c.bm) * std::ceil((double)t.in / c.bn), steps = std::ceil(R * e / kStepBytes);
         if (units > 1 << 22) continue;
@@ -698,7 +614,7 @@ HopProductPlan hopl_product_grad_plan(const HopProductGradTask& t, int dtype) {
             if (parts > 1 && (steps < 4 * parts || units * parts > 4 * kCus)) break;
             double us = kLaunch + 1.5 * (2 - i) + written / kHbm + steps_time(c, units * parts, std::ceil(steps / parts), 1.0);
             if (parts > 1) us += 3 + 2 * parts * written / kHbm;
-            if (us < least) least = us, best = {HOPL_STAGED, parts, i};
+            if (us < least) least = us, best = {fed ? HOPL_FED : HOPL_ANY, parts, i};
         }
     }
     return best;
@@ -706,42 +622,33 @@ HopProductPlan hopl_product_grad_plan(const HopProductGradTask& t, int dtype) {
 
 int hopl_product(const HopProductTask& t, const HopProductPlan& p, int dtype, int transposed, const HopIndex& index, void* stream) {
     hipStream_t st = (hipStream_t)stream;
-    const bool wide = dtype == HOP_BF16;
     if (p.kind == HOPL_FEW) {
-        if (wide) launch_few<bf16>(t, p.tile, index, st);
+        if (dtype == HOP_BF16) launch_few<bf16>(t, p.tile, index, st);
         else launch_few<float>(t, p.tile, index, st);
-    } else if (p.kind == HOPL_STAGED && wide) {
-        if (p.tile == 0) launch_staged<bf16, 256, 256, 2, 4>(t, transposed, p.parts, index, st);
-        else if (p.tile == 1) launch_staged<bf16, 128, 128, 2, 2>(t, transposed, p.parts, index, st);
-        else launch_staged<bf16, 32, 128, 1, 4>(t, transposed, p.parts, index, st);
-    } else if (p.kind == HOPL_STAGED) {
-        if (p.tile == 0) launch_staged<float, 128, 128, 2, 2>(t, transposed, p.parts, index, st);
-        else if (p.tile == 1) launch_staged<float, 64, 128, 2, 2>(t, transposed, p.parts, index, st);
-        else launch_staged<float, 32, 128, 1, 4>(t, transposed, p.parts, index, st);
+    } else if (dtype == HOP_BF16) {
+        if (p.tile == 0) launch_staged<bf16, true, 256, 256, 2, 4>(t, transposed, p.parts, index, st);
+        else if (p.kind == HOPL_FED) launch_tile<bf16, true>(t, transposed, p, index, st);
+        else launch_tile<bf16, false>(t, transposed, p, index, st);
     } else {
-        const dim3 grid((unsigned)pieces_of(t.rows, kTile), (unsigned)((t.out + kTile - 1) / kTile));
-        if (wide && transposed) product_kernel<bf16, true><<<grid, kThreads, 0, st>>>(t, index);
-        else if (wide) product_kernel<bf16, false><<<grid, kThreads, 0, st>>>(t, index);
-        else if (transposed) product_kernel<float, true><<<grid, kThreads, 0, st>>>(t, index);
-        else product_kernel<float, false><<<grid, kThreads, 0, st>>>(t, index);
+        if (p.kind == HOPL_FED) launch_tile<float, true>(t, transposed, p, index, st);
+        else launch_tile<float, false>(t, transposed, p, index, st);
     }
     return (int)hipGetLastError();
 }
 
 int hopl_product_grad(const HopProductGradTask& t, const HopProductPlan& p, int dtype, const HopIndex& index, void* stream) {
     hipStream_t st = (hipStream_t)stream;
-    const bool wide = dtype == HOP_BF16;
-    if (p.kind == HOPL_STAGED && wide) {
-        if (p.tile == 0) launch_grad_staged<bf16, 256, 256, 2, 4>(t, p.parts, index, st);
-        else if (p.tile == 1) launch_grad_staged<bf16, 128, 128, 2, 2>(t, p.parts, index, st);
-        else launch_grad_staged<bf16, 64, 64, 2, 2>(t, p.parts, index, st);
-    } else if (p.kind == HOPL_STAGED) {
-        if (p.tile == 0) launch_grad_staged<float, 128, 128, 2, 2>(t, p.parts, index, st);
-        else launch_grad_staged<float, 64, 64, 2, 2>(t, p.parts, index, st);
+    if (dtype == HOP_BF16) {
+        if (p.tile == 0) launch_grad_staged<bf16, true, 256, 256, 2, 4>(t, p.parts, index, st);
+        else if (p.kind == HOPL_FED && p.tile == 1) launch_grad_staged<bf16, true, 128, 128, 2, 2>(t, p.parts, index, st);
+        else if (p.kind == HOPL_FED) launch_grad_staged<bf16, true, 64, 64, 2, 2>(t, p.parts, index, st);
+        else if (p.tile == 1) launch_grad_staged<bf16, false, 128, 128, 2, 2>(t, p.parts, index, st);
+        else launch_grad_staged<bf16, false, 64, 64, 2, 2>(t, p.parts, index, st);
     } else {
-        const dim3 grid((unsigned)((t.in + kTile - 1) / kTile), (unsigned)((t.out + kTile - 1) / kTile), (unsigned)t.rows.G);
-        if (wide) product_grad_kernel<bf16><<<grid, kThreads, 0, st>>>(t, index);
-        else product_grad_kernel<float><<<grid, kThreads, 0, st>>>(t, index);
+        if (p.kind == HOPL_FED && p.tile == 0) launch_grad_staged<float, true, 128, 128, 2, 2>(t, p.parts, index, st);
+        else if (p.kind == HOPL_FED) launch_grad_staged<float, true, 64, 64, 2, 2>(t, p.parts, index, st);
+        else if (p.tile == 0) launch_grad_staged<float, false, 128, 128, 2, 2>(t, p.parts, index, st);
+        else launch_grad_staged<float, false, 64, 64, 2, 2>(t, p.parts, index, st);
     }
     return (int)hipGetLastError();
 }
