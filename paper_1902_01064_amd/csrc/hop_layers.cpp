@@ -12,6 +12,7 @@ namespace {
 
 constexpr uint64_t STREAM_DROPOUT = 8;         // beside hoprng's streams
 constexpr int64_t kMostRows = (1 << 30) - 65536;
+constexpr int64_t kMostDropCols = 1 << 29;     // a place in a row is a 32-bit number of bytes
 constexpr int64_t kMostCols = 1 << 21;         // a grid has room for 65535 tiles
 
 int hip_fail(hipError_t e, const char* what) {
@@ -51,14 +52,16 @@ bool drop_ok(const hop_drop* d) {
     return !d || (d->p >= 0.f && d->p <= 1.f && d->first_row >= 0 && d->first_row <= INT64_MAX - kMostRows);
 }
 HopMask mask_of(const hop_drop* d) {
-    HopMask m = {0, 0, 0, 0, 1.f};
+    HopMask m = {0, 0, 0, 0, 0, 1.f};
     if (!d) return m;
     const uint64_t key = hoprng::mix(d->seed, STREAM_DROPOUT, (uint64_t)(int64_t)d->worker, (uint64_t)(int64_t)d->iter, (uint64_t)(int64_t)d->site);
     m.k0 = (uint32_t)key;
     m.k1 = (uint32_t)(key >> 32);
     m.first_row = d->first_row;
-    m.threshold = (uint32_t)std::floor((double)d->p * 65536.0 + 0.5);
-    m.factor = m.threshold < 65536u ? (float)(65536.0 / (65536.0 - m.threshold)) : 0.f;
+    const uint32_t threshold = (uint32_t)std::floor((double)d->p * 65536.0 + 0.5);
+    m.none = threshold > 65535u;
+    m.threshold = m.none ? 0xFFFFFFFFu : threshold << 16;
+    m.factor = m.none ? 0.f : (float)(65536.0 / (65536.0 - threshold));
     return m;
 }
 
@@ -196,7 +199,7 @@ int hop_product_grad(const hop_product_grad_args* a, void* scratch, size_t scrat
 }
 
 int hop_dropout(int32_t dtype, const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int64_t cols, const hop_drop* drop, void* stream) {
-    if (!known_type(dtype) || !drop || !drop_ok(drop) || rows < 0 || rows > kMostRows || cols < 1 || cols > (int64_t)1 << 32) return HOP_ERR_INVALID_ARG;
+    if (!known_type(dtype) || !drop || !drop_ok(drop) || rows < 0 || rows > kMostRows || cols < 1 || cols > kMostDropCols) return HOP_ERR_INVALID_ARG;
     if (rows == 0) return HOP_OK;
     const size_t e = type_bytes(dtype);
     if (!matrix_ok(x, ldx, cols, e) || !matrix_ok(y, ldy, cols, e) || (x == y && ldx != ldy)) return HOP_ERR_INVALID_ARG;

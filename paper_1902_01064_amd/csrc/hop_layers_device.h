@@ -23,22 +23,22 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 // LDS counter).
 #define HOPL_GLOBAL __attribute__((address_space(1)))
 
+// The first n (1 <= n) of a vector's elements from p on, the rest zero: as many loads as the vector is long whatever n is, all at once -
+// behind branches each would wait for the one before.
+template <typename V, typename T>
+__device__ __forceinline__ V load_short(const T* p, int n) {
+    constexpr int kN = sizeof(V) / sizeof(T);
+    V v;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = ((const HOPL_GLOBAL T*)p)[i < n ? i : 0];
+#pragma unroll
+    for (int i = 1; i < kN; ++i) v[i] = i < n ? v[i] : (T)0.f;
+    return v;
+}
 // Eight consecutive elements from p on, as floats; the first n of them exist (n >= 8: all).
 __device__ __forceinline__ f32x8 load8(const float* p, int n) {
     if (n >= 8) return *(const HOPL_GLOBAL f32x8_any*)p;
-    f32x8 v = 0.f;
-#pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (i < n) v[i] = ((const HOPL_GLOBAL float*)p)[i];
-    return v;
-}
-__device__ __forceinline__ f32x8 load8(const bf16* p, int n) {
-    if (n >= 8) return __builtin_convertvector(*(const HOPL_GLOBAL bf16x8_any*)p, f32x8);
-    f32x8 v = 0.f;
-#pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (i < n) v[i] = (float)((const HOPL_GLOBAL bf16*)p)[i];
-    return v;
+    return load_short<f32x8>(p, n);
 }
 __device__ __forceinline__ void store8(float* p, int n, f32x8 v) {
     if (n >= 8) {

@@ -47,7 +47,8 @@ struct HopProductPlan {
 struct HopMask {                   // of a dropout: key, first row, threshold and factor
     uint32_t k0, k1;
     int64_t first_row;
-    uint32_t threshold;            // kept: draw >= threshold; 0: all
+    uint32_t threshold;            // kept: the draw's 16 bits, as the upper half of a word, are at least this; 0: all
+    int32_t none;                  // p = 1: nothing is kept, whatever the draw
     float factor;
 };
 

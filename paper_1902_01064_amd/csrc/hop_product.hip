@@ -123,9 +123,7 @@ struct RegisterFeed {
             if (off + kChunk <= end) {
                 part[i] = *(const HOPL_GLOBAL chunk_any*)p;
             } else {
-#pragma unroll
-                for (int e = 0; e < kChunk; ++e)
-                    if (e < n) part[i][e] = p[e];
+                part[i] = load_short<chunk>(base + off, n < kChunk ? n : kChunk);
             }
         }
     }
