@@ -616,6 +616,8 @@ void launch(const HopResidualTask& t, const HopIndex& index, int64_t pieces, boo
     else if (t.cols <= 1024) launch<T, 128, 1, EVEN>(t, index, pieces, grad, st);
     else if (t.cols <= 2048) launch<T, 256, 1, EVEN>(t, index, pieces, grad, st);
     else if (t.cols <= 4096) launch<T, 512, 1, EVEN>(t, index, pieces, grad, st);
+    else if (t.cols <= 6144) launch<T, 768, 1, EVEN>(t, index, pieces, grad, st);
+    else if (t.cols <= 8192 && !(grad && sizeof(T) == 4)) launch<T, 1024, 1, EVEN>(t, index, pieces, grad, st);
     else if (t.cols <= 8192) launch<T, 512, 2, EVEN>(t, index, pieces, grad, st);
     else if (t.cols <= 16384) launch<T, 1024, 2, EVEN>(t, index, pieces, grad, st);
     else launch<T, 1024, 4, EVEN>(t, index, pieces, grad, st);
