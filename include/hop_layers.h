@@ -26,6 +26,9 @@
  *  - Calls enqueue kernels on `stream` and return (no allocation, no copy, no wait); they can be captured into a HIP graph.
  *    `scratch` is device memory, 16-byte aligned, of at least the bytes that the matching *_scratch_bytes call names (which may
  *    be 0); it is free again when the call's kernels have run.  Results are the same bits on every call with the same arguments.
+ *  - Sizes: rows below 2^30 - 65536, products' columns up to 2^21, dropout's up to 2^29; anything else, like every null pointer, misaligned
+ *    address, distance below the columns, unknown enum value and index below zero, is HOP_ERR_INVALID_ARG and nothing is launched; too
+ *    little scratch is HOP_ERR_ARENA_TOO_SMALL.
  *  - No rows (rows = 0): nothing is written except the gradients of parameters, which are zero.
  */
 #ifndef HOP_LAYERS_H
@@ -39,7 +42,7 @@ extern "C" {
 
 #define HOP_MAX_GROUPS 4096        /* most groups of a call */
 #define HOP_MAX_INDEXED 256        /* most groups of a call with an index list */
-#define HOP_MAX_NORM_COLS 32768    /* widest row of hop_residual */
+#define HOP_MAX_NORM_COLS 32768    /* widest row of hop_residual; up to 16384 are what it is fast for */
 
 enum { HOP_F32 = 0, HOP_BF16 = 1 };
 /* none; x / sqrt(mean x^2 + eps); (x - mean x) / sqrt(var x + eps) */

@@ -1,6 +1,7 @@
 // C ABI of include/hop_layers.h: checks of arguments and their translation into what the kernels take.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -41,10 +42,11 @@ bool index_ok(const int32_t* index, int G) {
 }
 // two groups with the same row of a lattice would write the same gradient
 bool distinct(const int32_t* index, int G) {
-    for (int g = 0; index && g < G; ++g)
-        for (int h = 0; h < g; ++h)
-            if (index[g] == index[h]) return false;
-    return true;
+    if (!index) return true;
+    int32_t sorted[HOP_MAX_INDEXED];
+    std::copy(index, index + G, sorted);
+    std::sort(sorted, sorted + G);
+    return std::adjacent_find(sorted, sorted + G) == sorted + G;
 }
 HopRows rows_of(const hop_groups& g) { return HopRows{g.row_begin, g.G, (int32_t)g.rows}; }
 
@@ -171,7 +173,7 @@ int hop_product(const hop_product_args* a, void* scratch, size_t scratch_bytes, 
         if (scratch_bytes < (size_t)p.parts * (size_t)t.rows.rows * (size_t)t.out * 4) return HOP_ERR_ARENA_TOO_SMALL;
         t.partial = (float*)scratch;
     }
-    HopIndex index;
+    HopIndex index = {};
     hop_index_fill(&index, a->w_index, a->groups.G);
     const int rc = hopl_product(t, p, a->groups.dtype, a->transposed != 0, index, stream);
     return rc ? hip_fail((hipError_t)rc, "product launch") : HOP_OK;
@@ -192,7 +194,7 @@ int hop_product_grad(const hop_product_grad_args* a, void* scratch, size_t scrat
         if (scratch_bytes < (size_t)p.parts * (size_t)t.rows.G * (size_t)t.out * (size_t)t.in * 4) return HOP_ERR_ARENA_TOO_SMALL;
         t.partial = (float*)scratch;
     }
-    HopIndex index;
+    HopIndex index = {};
     hop_index_fill(&index, a->dw_index, a->groups.G);
     const int rc = hopl_product_grad(t, p, a->groups.dtype, index, stream);
     return rc ? hip_fail((hipError_t)rc, "product gradient launch") : HOP_OK;
@@ -218,7 +220,7 @@ int hop_residual(const hop_residual_args* a, const void* x, int64_t ldx, void* y
     t.x = x; t.ldx = ldx;
     t.y = y; t.ldy = ldy;
     t.h = h; t.ldh = ldh;
-    HopIndex index;
+    HopIndex index = {};
     hop_index_fill(&index, a->index, a->groups.G);
     const int rc = hopl_residual(t, a->groups.dtype, index, stream);
     return rc ? hip_fail((hipError_t)rc, "residual launch") : HOP_OK;
@@ -242,7 +244,7 @@ int hop_residual_grad(const hop_residual_args* a, const hop_residual_grads* g, v
     t.dpost_stride = g->dpost_stride; t.dpre_stride = g->dpre_stride; t.dgate_stride = g->dgate_stride;
     t.dindexed = g->index != nullptr;
     t.partial = need ? (float*)scratch : nullptr;
-    HopIndex index, dindex;
+    HopIndex index = {}, dindex = {};
     hop_index_fill(&index, a->index, a->groups.G);
     hop_index_fill(&dindex, g->index, a->groups.G);
     const int rc = hopl_residual_grad(t, a->groups.dtype, index, dindex, stream);

@@ -549,9 +549,11 @@ constexpr TileCost kGradTilesBf16[3] = {{256, 256, 64, 1.75, 1.1, 0.0, 1}, {128,
 constexpr TileCost kGradTilesF32[2] = {{128, 128, 32, 1.93, 2.1, 0.0, 2}, {64, 64, 32, 0.48, 0.65, 0.2, 4}};
 constexpr double kCus = 256, kHbm = 5.2e6, kJoin = 6e6, kLaunch = 4;       // bytes a us; us
 
-// Steps of `units` workgroups; `fill`: the part of a tile that is not padding.
-double steps_time(const TileCost& c, double units, double steps, double fill) {
-    const double each = std::max(1.0, std::ceil(units / kCus)), one = std::max(c.least, c.beside == 1 ? c.full * fill : 1.1 * c.full * fill);
+// Steps of `units` workgroups; `fill`: the part of a tile that is not padding; `far`: the weights are too many for the caches, which the
+// smaller tiles feel (2048 rows over 16 groups of 1024 x 4096 in bf16, transposed: 1.0 us a step of 128 x 128, 0.55 from the L2).
+double steps_time(const TileCost& c, double units, double steps, double fill, bool far) {
+    const double each = std::max(1.0, std::ceil(units / kCus));
+    const double one = std::max(c.least * (far && c.beside > 1 ? 1.6 : 1.0), c.beside == 1 ? c.full * fill : 1.1 * c.full * fill);
     return steps * std::max(std::ceil(each / c.beside) * one, each * c.full * fill) + each * c.own;
 }
 
@@ -572,13 +574,14 @@ HopProductPlan hopl_product_plan(const HopProductTask& t, int dtype, int transpo
     };
     for (int i = fed && dtype == HOP_BF16 ? 0 : 1; i < 4; ++i) {
         TileCost c = dtype == HOP_BF16 ? kTilesBf16[i] : kTilesF32[i];
+        if (!fed) c.full *= 1.2, c.least *= 1.4;       // through registers (4096 x 4096 x 4095 in fp32: 1166 us, 994 when fed)
         if (dtype == HOP_F32 && transposed && i == 2) c.full *= 1.15;          // its reads of single words from LDS (4096^3: 1157 us, 1000 the other way)
         if (pieces_of(t.rows, c.bm) * ((t.out + c.bn - 1) / c.bn) > 1 << 22) continue;
         const double per = R <= c.bm / 2 ? 1 : R / c.bm + 0.5, fill = std::min(1.0, (R + c.grain / 2) / (per * c.bm));
         const double units = G * per * std::ceil(out / c.bn), steps = std::ceil(in * e / kStepBytes);
         for (int parts = 1; parts <= 8; parts *= 2) {
-            if (parts > 1 && (steps < 2 * parts || units * parts > 4 * kCus)) break;
-            double us = kLaunch + together(bytes, steps_time(c, units * parts, std::ceil(steps / parts), fill));
+            if (parts > 1 && (steps < 2 * parts || units * parts > 10 * kCus)) break;
+            double us = kLaunch + together(bytes, steps_time(c, units * parts, std::ceil(steps / parts), fill, G * in * out * e > 64e6));
             if (parts > 1) us += 3 + parts * T * out * 8 / kJoin;
             consider(us, {fed ? HOPL_FED : HOPL_ANY, parts, i});
         }
@@ -586,7 +589,7 @@ HopProductPlan hopl_product_plan(const HopProductTask& t, int dtype, int transpo
     // Few rows: a turn of all wavefronts takes 1.25 us when nothing else is in its way; with 32 rows the weights come at 3 TB/s (64 rows of
     // 4096 x 4096 in bf16 26 us), with 16 at 5 (33 us).  Sixteen wavefronts where there are too few workgroups for four of them each (1 row, 8192 x 1024:
     // 14.2 -> 12.7 us; 8 rows over 8 groups of 1024 x 1024 6.6 -> 9.6).
-    if (fed && !transposed && R <= 64 && T * in * out < 1e12) {
+    if (fed && !transposed && R <= 128 && T * in * out < 1e12) {
         for (int wide = 0; wide < 2; ++wide) {
             const double pieces = G * std::max(1.0, R <= (wide ? 32 : 16) ? 1.0 : R / (wide ? 32 : 16) + 0.5), units = pieces * std::ceil(out / 16);
             const double turns = std::ceil(in * e / 2048.0);
@@ -609,8 +612,8 @@ HopProductPlan hopl_product_grad_plan(const HopProductGradTask& t, int dtype) {
         const double units = G * std::ceil((double)t.out / c.bm) * std::ceil((double)t.in / c.bn), steps = std::ceil(R * e / kStepBytes);
         if (units > 1 << 22) continue;
         for (int parts = 1; parts <= 8; parts *= 2) {
-            if (parts > 1 && (steps < 4 * parts || units * parts > 4 * kCus)) break;
-            double us = kLaunch + 1.5 * (2 - i) + written / kHbm + steps_time(c, units * parts, std::ceil(steps / parts), 1.0);
+            if (parts > 1 && (steps < 2 * parts || units * parts > 10 * kCus)) break;
+            double us = kLaunch + 1.5 * (2 - i) + written / kHbm + steps_time(c, units * parts, std::ceil(steps / parts), 1.0, false);
             if (parts > 1) us += 3 + 2 * parts * written / kHbm;
             if (us < least) least = us, best = {fed ? HOPL_FED : HOPL_ANY, parts, i};
         }

@@ -373,6 +373,27 @@ def test_dropped_places_take_nothing_from_a_gradient_that_is_no_number():
     assert torch.isfinite(y).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [8, 256, 1032, 4104, 6000])
+def test_any_alignment_gives_the_same_rows(dtype, cols):
+    """The same values at addresses and distances that are multiples of 16, 8, 4 and 2 bytes; rows of whole pieces of eight columns go
+    another way than others, sums in the same order."""
+    begin, x, b, z, dy, dh, y, post, pre, _, drop = residual_case(dtype, [5, 0, 30], cols, "rms", "centred", "element", True, True, 0.25, cols)
+    how = dict(row_begin=table(begin), norm="rms", post=post[0], scale=0.7, drop=drop, next_norm="centred", pre=pre[0], eps=1e-3)
+
+    def run(at, pad):
+        def moved(t):
+            return laid_out(t, pad, at)
+        out, _ = holes(35, cols, dtype, pad, at)
+        layers.residual(moved(x[0]), moved(b[0]), gate_logits=moved(z[0]), out=out, **how)
+        g = layers.residual_grad(moved(dy[0]), moved(dh[0]), moved(y[0]), moved(b[0]), gate_logits=moved(z[0]), **how)
+        return [out.clone(), *[t for t in g if t is not None], layers.dropout(moved(x[0]), drop)]
+    want = run(0, 0)
+    for at, pad in ((8, 8), (4, 4), (2, 2), (1, 0), (0, 1), (3, 5)):
+        for a, c in zip(want, run(at, pad)):
+            assert torch.allclose(a.float(), c.float(), rtol=2.0 ** -7 if dtype == "bf16" else 1e-5, atol=1e-5), (at, pad)
+
+
 # --------------------------------------------------------------------- streams, graphs, the same bits ----
 def everything(x, b, w, w2, vec, rb, drop):
     h = layers.norm(x, vec, rb)
