@@ -169,8 +169,8 @@ int hop_product(const hop_product_args* a, void* scratch, size_t scratch_bytes, 
     HopProductTask t = product_task(a);
     const HopProductPlan p = hopl_product_plan(t, a->groups.dtype, a->transposed != 0);
     if (p.parts > 1) {
-        if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
         if (scratch_bytes < (size_t)p.parts * (size_t)t.rows.rows * (size_t)t.out * 4) return HOP_ERR_ARENA_TOO_SMALL;
+        if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
         t.partial = (float*)scratch;
     }
     HopIndex index = {};
@@ -190,8 +190,8 @@ int hop_product_grad(const hop_product_grad_args* a, void* scratch, size_t scrat
     HopProductGradTask t = product_grad_task(a);
     const HopProductPlan p = hopl_product_grad_plan(t, a->groups.dtype);
     if (p.parts > 1) {
-        if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
         if (scratch_bytes < (size_t)p.parts * (size_t)t.rows.G * (size_t)t.out * (size_t)t.in * 4) return HOP_ERR_ARENA_TOO_SMALL;
+        if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
         t.partial = (float*)scratch;
     }
     HopIndex index = {};
@@ -234,8 +234,8 @@ size_t hop_residual_grad_scratch_bytes(const hop_residual_args* a, const hop_res
 int hop_residual_grad(const hop_residual_args* a, const hop_residual_grads* g, void* scratch, size_t scratch_bytes, void* stream) {
     if (!grads_ok(a, g)) return HOP_ERR_INVALID_ARG;
     const size_t need = hop_residual_grad_scratch_bytes(a, g);
-    if (need && (!scratch || ((uintptr_t)scratch & 15u))) return HOP_ERR_INVALID_ARG;
     if (scratch_bytes < need) return HOP_ERR_ARENA_TOO_SMALL;
+    if (need && (!scratch || ((uintptr_t)scratch & 15u))) return HOP_ERR_INVALID_ARG;
     HopResidualTask t = residual_task(a);
     t.dy = g->dy; t.dh = g->dh; t.y = const_cast<void*>(g->y);
     t.dx = g->dx; t.db = g->db; t.dz = g->dz;

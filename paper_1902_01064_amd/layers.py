@@ -156,8 +156,16 @@ def _weights(w, name, gpu):
     return stride[0], max(stride[1], shape[2]), shape
 
 
-def _scratch(nbytes, like):
-    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+def _with_scratch(name, like, gpu, *args):
+    """The call, with scratch if it says that it needs some (most do not, and asking each of them first would cost another call)."""
+    lib = _lib or load()
+    rc = getattr(lib, name)(*args, None, 0, _raw_stream(gpu))
+    if rc == hop.HOP_ERR_ARENA_TOO_SMALL:
+        need = getattr(lib, name + "_scratch_bytes")(*args)
+        s = like.new_empty(need, dtype=torch.uint8)
+        rc = getattr(lib, name)(*args, s.data_ptr(), need, _raw_stream(gpu))
+    if rc:
+        hop._check(rc, name)
 
 
 def _drop(drop):
@@ -186,10 +194,7 @@ def product(x, w, row_begin=None, index=None, transposed=False, out=None):
         ldy = _ld(out, "out", x.dtype, gpu, rows, a)
     args = _PRODUCT(rows, table, G, dtype, x.data_ptr(), ldx, w.data_ptr(), ldw, step, _address(idx), out.data_ptr(), ldy, k, a,
                     1 if transposed else 0, 0)
-    lib = load()
-    need = lib.hop_product_scratch_bytes(args)
-    s = _scratch(need, x)
-    hop._check(lib.hop_product(args, s.data_ptr() if need else None, need, _raw_stream(gpu)), "hop_product")
+    _with_scratch("hop_product", x, gpu, args)
     return out
 
 
@@ -210,10 +215,7 @@ def product_grad(dy, x, row_begin=None, out=None, index=None):
     step, lddw, (M, _, _) = _weights(out, "out", gpu)
     idx = _index(index, G, M, "out")
     args = _PRODUCT_GRAD(rows, table, G, dtype, dy.data_ptr(), lddy, x.data_ptr(), ldx, out.data_ptr(), lddw, step, _address(idx), k, n)
-    lib = load()
-    need = lib.hop_product_grad_scratch_bytes(args)
-    s = _scratch(need, x)
-    hop._check(lib.hop_product_grad(args, s.data_ptr() if need else None, need, _raw_stream(gpu)), "hop_product_grad")
+    _with_scratch("hop_product_grad", x, gpu, args)
     return out
 
 
@@ -225,7 +227,7 @@ def dropout(x, drop, out=None):
         out, ldy = x.new_empty((rows, cols)), cols
     else:
         ldy = _ld(out, "out", x.dtype, gpu, rows, cols)
-    hop._check(load().hop_dropout(dtype, x.data_ptr(), ldx, out.data_ptr(), ldy, rows, cols, _drop(drop), _raw_stream(gpu)), "hop_dropout")
+    hop._check((_lib or load()).hop_dropout(dtype, x.data_ptr(), ldx, out.data_ptr(), ldy, rows, cols, _drop(drop), _raw_stream(gpu)), "hop_dropout")
     return out
 
 
@@ -273,7 +275,7 @@ def residual(x, b, row_begin=None, index=None, norm="rms", post=None, gate=None,
     args, keep, _ = _residual_args(rows, cols, dtype, x.dtype, gpu, b, row_begin, index, norm, post, gate, gate_logits, scale, drop, next_norm, pre, eps)
     y, y_at, ldy = _result(out, x, "out", gpu, rows, cols)
     h, h_at, ldh = (None, None, 0) if next_norm is None else _result(out_next, x, "out_next", gpu, rows, cols)
-    hop._check(load().hop_residual(args, x.data_ptr(), ldx, y_at, ldy, h_at, ldh, _raw_stream(gpu)), "hop_residual")
+    hop._check((_lib or load()).hop_residual(args, x.data_ptr(), ldx, y_at, ldy, h_at, ldh, _raw_stream(gpu)), "hop_residual")
     del keep
     return y, h
 
@@ -283,7 +285,7 @@ def norm(x, pre=None, row_begin=None, index=None, norm="rms", eps=1e-5, out=None
     dtype, gpu, ldx, rows, cols = _rows(x, "x")
     args, keep, _ = _residual_args(rows, cols, dtype, x.dtype, gpu, None, row_begin, index, None, None, None, None, 1.0, None, norm, pre, eps)
     h, h_at, ldh = _result(out, x, "out", gpu, rows, cols)
-    hop._check(load().hop_residual(args, x.data_ptr(), ldx, None, 0, h_at, ldh, _raw_stream(gpu)), "hop_residual")
+    hop._check((_lib or load()).hop_residual(args, x.data_ptr(), ldx, None, 0, h_at, ldh, _raw_stream(gpu)), "hop_residual")
     del keep
     return h
 
@@ -330,10 +332,7 @@ def residual_grad(dy, dh, y, b, row_begin=None, index=None, norm="rms", post=Non
         packed += [at, step]
     idx = None if M is None else _index(grad_index, G, M, "dpost, dpre, dgate")
     out = _GRADS(dy_at, lddy, dh_at, lddh, y_at, ldy, dx_at, lddx, db_at, lddb, dz_at, lddz, *packed, _address(idx))
-    lib = load()
-    need = lib.hop_residual_grad_scratch_bytes(args, out)
-    s = _scratch(need, like)
-    hop._check(lib.hop_residual_grad(args, out, s.data_ptr() if need else None, need, _raw_stream(gpu)), "hop_residual_grad")
+    _with_scratch("hop_residual_grad", like, gpu, args, out)
     del keep
     return ResidualGrads(dx, db, *grads, dlogits)
 
