@@ -82,5 +82,5 @@ int hopl_residual(HopResidualTask t, int dtype, const HopIndex& index, void* str
 int hopl_residual_grad(HopResidualTask t, int dtype, const HopIndex& index, const HopIndex& dindex, void* stream);
 
 // Rows of a chunk of the gradient (as a power of two) and how many chunks its partial sums need room for.
-int hopl_grad_shift(int64_t rows, int G, int64_t cols);
+int hopl_grad_shift(int64_t rows, int64_t cols);
 int64_t hopl_grad_chunks(int64_t rows, int G, int64_t cols);

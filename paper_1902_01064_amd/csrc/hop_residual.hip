@@ -4,9 +4,9 @@
 //   e = dy + next_norm'(dh pre; y), f = scale dropout(e), q = f gate, db = norm'(q post; b), norm'(a; v) = r (a - [mean a] - n mean(a n))
 //
 // A row is read once, stays in registers through its statistics (eight consecutive columns a thread), and is written once; the mask is worked
-// out again wherever it is needed.  About 45 vector instructions an element forwards and 65 back (a third of them the generator), so instruction issue
-// comes close behind the bytes: 16384 x 4096 in bf16 with dropout 104 us forwards (5.2 TB/s of the 537 MB), 177 back (4.5 TB/s of 805); dropout
-// of 8192 x 8192 in bf16 48 us (5.6 TB/s).  With few rows the chain of a row - loads, two to four sums over the workgroup - bounds it: 8 rows of 4096 5.6 us.
+// out again wherever it is needed.  About 39 vector instructions an element forwards and 54 back, the generator's among them, so instruction issue comes
+// close behind the bytes: 16384 x 4096 in bf16 with dropout 103 us forwards (5.2 TB/s of the 537 MB), 170 back (4.7 TB/s of 805); dropout of
+// 8192 x 8192 in bf16 48 us (5.6 TB/s).  With few rows the chain of a row - loads, two to four sums over the workgroup - bounds it: 8 rows of 4096 5.6 us.
 #include <type_traits>
 
 #include "hop_layers_device.h"
@@ -237,7 +237,7 @@ __device__ __forceinline__ f32x8 logistic(f32x8 z) {
 
 // The vectors of a group that a workgroup needs for all its rows wait in LDS, each thread's own columns (so there is no barrier), while that
 // has room for them: 12 bytes a column, rows of up to 8192.  In registers they would take the place of rows under way.
-template <int NT, int V, int N>
+template <int NT, int V>
 struct Vectors {
     static constexpr bool kKept = NT * V <= 1024;
     f32x4 (*kept)[2 * V][kKept ? NT : 1];
@@ -255,7 +255,7 @@ struct Vectors {
 // row's loads are on their way while a row's statistics are worked out.
 template <typename T, int NT, int V, bool EVEN>
 __global__ __launch_bounds__(NT) void residual_kernel(HopResidualTask t, HopIndex index) {
-    typedef Vectors<NT, V, 2> Vec;
+    typedef Vectors<NT, V> Vec;
     __shared__ float shared[4 * (NT / 64)];
     __shared__ f32x4 kept[Vec::kKept ? 2 : 1][2 * V][Vec::kKept ? NT : 1];
     RowSums<NT> sums{shared, 0};
@@ -662,15 +662,14 @@ int hopl_residual(HopResidualTask t, int dtype, const HopIndex& index, void* str
 
 // Gradient: a piece's sums have to be joined with the others', so few rows go in few pieces too (512 x 2048 in bf16: 512 pieces 26 us, 256 19;
 // 16384 x 4096: 1024 pieces 207 us, 512 182, 256 172; 16384 x 1024: 2048 pieces 82 us, 1024 63).
-int hopl_grad_shift(int64_t rows, int G, int64_t cols) {
-    (void)G;
+int hopl_grad_shift(int64_t rows, int64_t cols) {
     return shift_for(rows, cols <= 1024 ? 768 : cols <= 2048 ? 256 : 192);
 }
-int64_t hopl_grad_chunks(int64_t rows, int G, int64_t cols) { return pieces_of(rows, G, hopl_grad_shift(rows, G, cols)); }
+int64_t hopl_grad_chunks(int64_t rows, int G, int64_t cols) { return pieces_of(rows, G, hopl_grad_shift(rows, cols)); }
 
 int hopl_residual_grad(HopResidualTask t, int dtype, const HopIndex& index, const HopIndex& dindex, void* stream) {
     hipStream_t st = (hipStream_t)stream;
-    t.shift = hopl_grad_shift(t.rows.rows, t.rows.G, t.cols);
+    t.shift = hopl_grad_shift(t.rows.rows, t.cols);
     const int64_t chunks = pieces_of(t.rows.rows, t.rows.G, t.shift);
     if (chunks > 0) {
         if (dtype == HOP_BF16) launch<bf16>(t, index, chunks, true, st);
