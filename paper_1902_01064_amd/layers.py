@@ -321,18 +321,31 @@ def residual_grad(dy, dh, y, b, row_begin=None, index=None, norm="rms", post=Non
     dlogits, dz_at, lddz = matrix(dlogits, "dlogits", gate_logits is not None)
     M, packed = None, []
     grads = [dpost, dpre, dgate]
-    for i, (name, p) in enumerate((("dpost", post), ("dpre", pre if dh is not None else None), ("dgate", gate))):
-        if p is None and grads[i] is not None:
-            raise ValueError("%s: there is nothing to differentiate" % name)
-        if p is not None and grads[i] is None:
-            if grad_index is not None:
-                raise ValueError("grad_index without %s" % name)
-            grads[i] = like.new_empty((G, cols), dtype=torch.float32)
-        at, step, M = _vector(grads[i], name, cols, gpu, M)
-        packed += [at, step]
+    params = (post, pre if dh is not None else None, gate)
+    if dpost is dpre is dgate is None and grad_index is None:          # new ones: parts of one allocation, nothing to check
+        wanted = [i for i in range(3) if params[i] is not None]
+        if wanted:
+            M = G
+            for i, t in zip(wanted, like.new_empty((len(wanted), G, cols), dtype=torch.float32).unbind(0)):
+                grads[i] = t
+        for t in grads:
+            packed += (0, 0) if t is None else (t.data_ptr(), cols)
+    else:
+        for i, name in enumerate(("dpost", "dpre", "dgate")):
+            if params[i] is None and grads[i] is not None:
+                raise ValueError("%s: there is nothing to differentiate" % name)
+            if params[i] is not None and grads[i] is None:
+                if grad_index is not None:
+                    raise ValueError("grad_index without %s" % name)
+                grads[i] = like.new_empty((G, cols), dtype=torch.float32)
+            at, step, M = _vector(grads[i], name, cols, gpu, M)
+            packed += (at, step)
     idx = None if M is None else _index(grad_index, G, M, "dpost, dpre, dgate")
     out = _GRADS(dy_at, lddy, dh_at, lddh, y_at, ldy, dx_at, lddx, db_at, lddb, dz_at, lddz, *packed, _address(idx))
-    _with_scratch("hop_residual_grad", like, gpu, args, out)
+    lib = _lib or load()
+    need = 0 if M is None else lib.hop_residual_grad_scratch_bytes(args, out)
+    scratch = like.new_empty(need, dtype=torch.uint8) if need else None
+    hop._check(lib.hop_residual_grad(args, out, scratch.data_ptr() if need else None, need, _raw_stream(gpu)), "hop_residual_grad")
     del keep
     return ResidualGrads(dx, db, *grads, dlogits)
 
