@@ -9,6 +9,7 @@ hop_step then reduces and applies them.
     python -m paper_1902_01064_amd.block [--workers 16] [--width 256] [--hidden 1024] [--iterations 60]
 """
 import argparse
+import contextlib
 
 import torch
 
@@ -89,6 +90,7 @@ class Training:
         c = dict(in_nbrs=in_nbrs, W=inputs.uniform_weights(in_nbrs), N=N, d=block.d, s=s, b=b, max_ig=0, skip_on=False, max_skip=10, trigger=1,
                  lr=lr, lam=0.0, batch=batch, seed=seed, momentum=momentum, model="external", K=K, delay_kind=delay_kind, mult=mult)
         self.session = sess = Session(c, device)
+        self.stream = torch.cuda.current_stream(sess.dev)                # the one that the session took
         self.x = torch.stack([x for x, _ in data]).to(sess.dev)
         self.target = torch.stack([t for _, t in data]).to(sess.dev)
         self.external = torch.zeros(N, block.d, device=sess.dev)
@@ -106,8 +108,30 @@ class Training:
         base = self.session.arena.data_ptr()
         return [(hop.hop_params(self.session.ctx, w)[0] - base) // (4 * self.session.stride) for w in workers]
 
+    @contextlib.contextmanager
+    def _session_stream(self):
+        """Layers read the rings that hop_step writes and write the gradients that it reads, so they run where it does, on the session's stream:
+        behind what the caller's stream holds now, and before what comes there next.  Yields the caller's stream."""
+        caller = torch.cuda.current_stream(self.session.dev)
+        if caller == self.stream:
+            yield caller
+            return
+        self.stream.wait_stream(caller)
+        try:
+            with torch.cuda.stream(self.stream):
+                yield caller
+        finally:
+            caller.wait_stream(self.stream)
+
     def wave(self, w):
         """One wave: gradients of its workers, then hop_step.  Returns the mean loss over its minibatches (on the GPU), or None."""
+        with self._session_stream() as caller:
+            loss = self._wave(w)
+            if loss is not None:
+                loss.record_stream(caller)
+        return loss
+
+    def _wave(self, w):
         sched = self.schedule
         records = [e for e in sched.wave_order[sched.wave_begin[w]:sched.wave_begin[w + 1]] if sched.kind[e] == hop.HOP_STEP]
         loss = None
@@ -127,6 +151,12 @@ class Training:
 
     def evaluate(self, x, target):
         """Mean loss of every worker's newest replica on the same samples, without dropout."""
+        with self._session_stream() as caller:
+            loss = self._evaluate(x, target)
+            loss.record_stream(caller)
+        return loss
+
+    def _evaluate(self, x, target):
         N = len(self.external)
         begin = torch.arange(0, (N + 1) * len(x), len(x), dtype=torch.int32, device=self.x.device)
         out, _ = self.block.forward(self.params, self.versions(range(N)), x.to(self.x.device).repeat(N, 1), begin, train=False)
