@@ -21,6 +21,8 @@
  *  - Parameters of group g: element 0 at base + (index ? index[g] : g) * stride elements.  For replicas in a context's arena the
  *    base is the arena plus the layer's place in the vector, the stride that of hop_layout, and index[g] = worker * depth + slot.
  *    `index` is host memory, read during the call.
+ *    Gradients of parameters go to different places for different groups: no number twice in their index, and the groups' matrices (vectors)
+ *    lie behind each other or row by row side by side; a distance that has them overlap is refused.
  *  - row_begin is device memory, G + 1 ascending row numbers from 0 to `rows`; a group may have none.  Kernels hold every row
  *    number they read against `rows` and touch nothing outside the tensors; what a table that breaks the rule gives is not specified.
  *  - Calls enqueue kernels on `stream` and return (no allocation, no copy, no wait); they can be captured into a HIP graph.

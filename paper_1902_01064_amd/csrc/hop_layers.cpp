@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 
 #include "hop_internal.h"
@@ -48,6 +49,15 @@ bool distinct(const int32_t* index, int G) {
     std::sort(sorted, sorted + G);
     return std::adjacent_find(sorted, sorted + G) == sorted + G;
 }
+// Whether the groups' gradients lie apart: matrices of `rows` rows `ld` apart, of `cols` columns, `stride` from group to group.  Either a group
+// lies behind the other, or their rows lie side by side within a row's distance.
+bool apart(const int32_t* index, int G, int64_t stride, int64_t rows, int64_t ld, int64_t cols) {
+    if (G < 2) return true;
+    const int64_t s = std::abs(stride);
+    if (rows == 1 ? s >= cols : s >= (rows - 1) * ld + cols) return true;
+    const int64_t span = index ? (int64_t)*std::max_element(index, index + G) - *std::min_element(index, index + G) : G - 1;
+    return s >= cols && span <= (ld - cols) / s;
+}
 HopRows rows_of(const hop_groups& g) { return HopRows{g.row_begin, g.G, (int32_t)g.rows}; }
 
 bool drop_ok(const hop_drop* d) {
@@ -87,7 +97,7 @@ bool product_grad_ok(const hop_product_grad_args* a) {
     if (!a || !groups_ok(a->groups, a->dw_index != nullptr) || a->in < 1 || a->in > kMostCols || a->out < 1 || a->out > kMostCols) return false;
     const size_t e = type_bytes(a->groups.dtype);
     return matrix_ok(a->dw, a->lddw, a->in, 4) && vectors_ok(nullptr, a->dw_stride) && index_ok(a->dw_index, a->groups.G) &&
-           distinct(a->dw_index, a->groups.G) &&
+           distinct(a->dw_index, a->groups.G) && apart(a->dw_index, a->groups.G, a->dw_stride, a->out, a->lddw, a->in) &&
            (a->groups.rows == 0 || (matrix_ok(a->dy, a->lddy, a->out, e) && matrix_ok(a->x, a->ldx, a->in, e)));
 }
 
@@ -150,7 +160,9 @@ bool grads_ok(const hop_residual_args* a, const hop_residual_grads* g) {
     if (rows && !a->b && (g->db || g->dpost || g->dgate || g->dz)) return false;
     if ((g->dpost && !a->post) || (g->dpre && !a->pre) || (g->dgate && !a->gate) || (g->dz && a->gate_kind != HOP_GATE_ELEMENT)) return false;
     if (g->index && a->groups.G > HOP_MAX_INDEXED) return false;
-    return index_ok(g->index, a->groups.G) && distinct(g->index, a->groups.G);
+    if (!index_ok(g->index, a->groups.G) || !distinct(g->index, a->groups.G)) return false;
+    auto vectors_apart = [&](const float* p, int64_t stride) { return !p || apart(g->index, a->groups.G, stride, 1, d, d); };
+    return vectors_apart(g->dpost, g->dpost_stride) && vectors_apart(g->dpre, g->dpre_stride) && vectors_apart(g->dgate, g->dgate_stride);
 }
 
 }  // namespace
