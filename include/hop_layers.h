@@ -17,7 +17,8 @@
  *    bfloat16 (`dtype`); norms' and gates' parameters and all gradients of parameters are fp32.  Pointers need the alignment of an element; the
  *    fastest forms want addresses and distances that are multiples of 16 bytes.
  *  - Sums, statistics and everything between reading and writing are held in fp32; what is written as bfloat16 is rounded once.
- *  - Outputs may not overlap inputs or each other, except that hop_dropout may work in place and that y of hop_residual may be x or b.
+ *  - Outputs may not overlap inputs or each other, except that hop_dropout may work in place and that y of hop_residual may be
+ *    x or b, with the same distance between rows.
  *  - Parameters of group g: element 0 at base + (index ? index[g] : g) * stride elements.  For replicas in a context's arena the
  *    base is the arena plus the layer's place in the vector, the stride that of hop_layout, and index[g] = worker * depth + slot.
  *    `index` is host memory, read during the call.

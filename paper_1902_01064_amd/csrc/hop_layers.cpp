@@ -228,6 +228,8 @@ int hop_residual(const hop_residual_args* a, const void* x, int64_t ldx, void* y
     if (!matrix_ok(x, ldx, a->cols, e) || (a->b ? !matrix_ok(y, ldy, a->cols, e) : y != nullptr) ||
         (a->next_norm ? !matrix_ok(h, ldh, a->cols, e) : h != nullptr))
         return HOP_ERR_INVALID_ARG;
+    // in place, row by row: at another distance a row would be written before another workgroup has read the row that lies there
+    if (a->groups.rows > 1 && y && ((y == x && ldy != ldx) || (y == a->b && ldy != a->ldb))) return HOP_ERR_INVALID_ARG;
     HopResidualTask t = residual_task(a);
     t.x = x; t.ldx = ldx;
     t.y = y; t.ldy = ldy;
