@@ -46,37 +46,60 @@ class ResidualBlock:
                 p[at:at + n] = 1.0 if name != "gate" else 0.5
         return p
 
-    def _drop(self, p, seed, it, site):
-        return layers.Drop(p, seed, 0, it, site) if p else None
+    def forward(self, params, index, x, row_begin, seed=0, it=0, train=True, draws=None):
+        """The block's output and what its gradient needs again.
 
-    def forward(self, params, index, x, row_begin, seed=0, it=0, train=True):
-        """The block's output and what its gradient needs again."""
+        Masks are drawn for all rows together, from worker 0 and iteration `it`; with `draws`, [(worker, iteration, rows)] of every group
+        (whose rows row_begin has to agree with), for each group from its worker and iteration, so they do not depend on which other groups there are.
+        A call of the layers has one mask, so the calls that drop are then made group by group."""
         p = self.p if train else 0.0
-        drop1, drop2 = self._drop(p, seed, it, 1), self._drop(p, seed, it, 2)
+        drops, groups = [(None, None)], [(x.shape[0], index, row_begin)]
+        if p and draws is None:
+            drops = [self._drops(p, seed, 0, it)]
+        elif p:
+            G = 1 if row_begin is None else row_begin.shape[0] - 1
+            if len(draws) != G or sum(rows for _, _, rows in draws) != x.shape[0]:
+                raise ValueError("draws: %d rows in %d groups are needed, got %s" % (x.shape[0], G, draws[:4]))
+            drops = [self._drops(p, seed, worker, iteration) for worker, iteration, _ in draws]
+            groups = [(rows, [i if index is None else index[i]], None) for i, (_, _, rows) in enumerate(draws)]
+        sizes = [rows for rows, _, _ in groups]
         h = layers.norm(x, params["pre"], row_begin, index, eps=self.eps)
         u = layers.product(h, params["w1"], row_begin, index)
         a = torch.relu(u)
-        if drop1:
-            a = layers.dropout(a, drop1)
+        if p:
+            self._dropout(a, sizes, drops)
         v = layers.product(a, params["w2"], row_begin, index)
-        y, out = layers.residual(x, v, row_begin, index, post=params["post"], gate=params["gate"], scale=self.scale, drop=drop2, next_norm="rms",
-                                 pre=params["head"], eps=self.eps)
-        return out, (x, h, u, a, v, y, drop1, drop2)
+        y, out = torch.empty_like(x), torch.empty_like(x)
+        how = dict(post=params["post"], gate=params["gate"], scale=self.scale, next_norm="rms", pre=params["head"], eps=self.eps)
+        for (_, where, begin), (_, drop), *t in zip(groups, drops, *(m.split(sizes) for m in (x, v, y, out))):
+            layers.residual(t[0], t[1], begin, where, drop=drop, out=t[2], out_next=t[3], **how)
+        return out, (x, h, u, a, v, y, groups, drops)
+
+    def _drops(self, p, seed, worker, iteration):
+        return layers.Drop(p, seed, worker, iteration, 1), layers.Drop(p, seed, worker, iteration, 2)
+
+    def _dropout(self, a, sizes, drops):
+        for part, (drop, _) in zip(a.split(sizes), drops):
+            layers.dropout(part, drop, out=part)
 
     def backward(self, params, index, saved, dout, row_begin, grads, grad_index):
         """Writes the gradients of all parameters into the rows grad_index of `grads`; returns the gradient of x."""
-        x, h, u, a, v, y, drop1, drop2 = saved
-        g = layers.residual_grad(None, dout, y, v, row_begin, index, post=params["post"], gate=params["gate"], scale=self.scale, drop=drop2,
-                                 next_norm="rms", pre=params["head"], eps=self.eps, dpost=grads["post"], dpre=grads["head"], dgate=grads["gate"],
-                                 grad_index=grad_index)
-        layers.product_grad(g.db, a, row_begin, out=grads["w2"], index=grad_index)
-        da = layers.product(g.db, params["w2"], row_begin, index, transposed=True)
-        if drop1:
-            da = layers.dropout(da, drop1)
+        x, h, u, a, v, y, groups, drops = saved
+        sizes = [rows for rows, _, _ in groups]
+        dy, db = torch.empty_like(x), torch.empty_like(x)
+        how = dict(post=params["post"], gate=params["gate"], scale=self.scale, next_norm="rms", pre=params["head"], eps=self.eps, dpost=grads["post"],
+                   dpre=grads["head"], dgate=grads["gate"])
+        to = [grad_index] if len(groups) == 1 else [[i if grad_index is None else grad_index[i]] for i in range(len(groups))]
+        for (_, where, begin), (_, drop), i, *t in zip(groups, drops, to, *(m.split(sizes) for m in (dout, y, v, dy, db))):
+            layers.residual_grad(None, t[0], t[1], t[2], begin, where, drop=drop, grad_index=i, dx=t[3], db=t[4], **how)
+        layers.product_grad(db, a, row_begin, out=grads["w2"], index=grad_index)
+        da = layers.product(db, params["w2"], row_begin, index, transposed=True)
+        if drops[0][0]:
+            self._dropout(da, sizes, drops)
         da = da * (u > 0)
         layers.product_grad(da, h, row_begin, out=grads["w1"], index=grad_index)
         dh = layers.product(da, params["w1"], row_begin, index, transposed=True)
-        dx, _ = layers.norm_grad(dh, x, params["pre"], row_begin, index, eps=self.eps, dy=g.dx, dpre=grads["pre"], grad_index=grad_index)
+        dx, _ = layers.norm_grad(dh, x, params["pre"], row_begin, index, eps=self.eps, dy=dy, dpre=grads["pre"], grad_index=grad_index)
         return dx
 
 
@@ -127,7 +150,7 @@ class Training:
         """One wave: gradients of its workers, then hop_step.  Returns the mean loss over its minibatches (on the GPU), or None."""
         with self._session_stream() as caller:
             loss = self._wave(w)
-            if loss is not None:
+            if loss is not None and caller != self.stream:
                 loss.record_stream(caller)
         return loss
 
@@ -142,7 +165,8 @@ class Training:
             x, target = self.x[who, at].flatten(0, 1), self.target[who, at].flatten(0, 1)
             begin = torch.arange(0, x.shape[0] + 1, self.batch, dtype=torch.int32, device=x.device)
             index = self.versions(workers)
-            out, saved = self.block.forward(self.params, index, x, begin, self.seed, w)
+            draws = [(int(sched.worker[e]), int(sched.iter[e]), self.batch) for e in records]
+            out, saved = self.block.forward(self.params, index, x, begin, self.seed, draws=draws)
             diff = out - target
             loss = diff.square().mean() / 2
             self.block.backward(self.params, index, saved, diff / (self.batch * self.block.width), begin, self.grads, workers)
@@ -153,7 +177,8 @@ class Training:
         """Mean loss of every worker's newest replica on the same samples, without dropout."""
         with self._session_stream() as caller:
             loss = self._evaluate(x, target)
-            loss.record_stream(caller)
+            if caller != self.stream:
+                loss.record_stream(caller)
         return loss
 
     def _evaluate(self, x, target):
