@@ -103,6 +103,11 @@ class ResidualBlock:
         return dx
 
 
+def _runs(items):
+    """Workers in runs of as many groups as a call with an index takes."""
+    return [items[i:i + layers.HOP_MAX_INDEXED] for i in range(0, len(items), layers.HOP_MAX_INDEXED)]
+
+
 class Training:
     """Workers on a graph that learn a block from their own samples (x, target), [samples, width] each."""
 
@@ -157,21 +162,26 @@ class Training:
     def _wave(self, w):
         sched = self.schedule
         records = [e for e in sched.wave_order[sched.wave_begin[w]:sched.wave_begin[w + 1]] if sched.kind[e] == hop.HOP_STEP]
-        loss = None
-        if records:
-            workers = [int(sched.worker[e]) for e in records]
-            at = torch.from_numpy(sched.batch_rows[records].astype("int64")).to(self.x.device)
-            who = torch.tensor(workers, device=self.x.device)[:, None]
-            x, target = self.x[who, at].flatten(0, 1), self.target[who, at].flatten(0, 1)
-            begin = torch.arange(0, x.shape[0] + 1, self.batch, dtype=torch.int32, device=x.device)
-            index = self.versions(workers)
-            draws = [(int(sched.worker[e]), int(sched.iter[e]), self.batch) for e in records]
-            out, saved = self.block.forward(self.params, index, x, begin, self.seed, draws=draws)
-            diff = out - target
-            loss = diff.square().mean() / 2
-            self.block.backward(self.params, index, saved, diff / (self.batch * self.block.width), begin, self.grads, workers)
+        losses = [(self._gradients(run), len(run)) for run in _runs(records)]
         hop.hop_step(self.session.ctx, sched, w, w + 1)
-        return loss
+        if len(losses) < 2:
+            return losses[0][0] if losses else None
+        return sum(loss * (n / len(records)) for loss, n in losses)
+
+    def _gradients(self, records):
+        """Gradients of the records' workers into their rows of `external`; mean loss."""
+        sched = self.schedule
+        draws = [(int(sched.worker[e]), int(sched.iter[e]), self.batch) for e in records]
+        workers = [worker for worker, _, _ in draws]
+        at = torch.from_numpy(sched.batch_rows[records].astype("int64")).to(self.x.device)
+        who = torch.tensor(workers, device=self.x.device)[:, None]
+        x, target = self.x[who, at].flatten(0, 1), self.target[who, at].flatten(0, 1)
+        begin = torch.arange(0, x.shape[0] + 1, self.batch, dtype=torch.int32, device=x.device)
+        index = self.versions(workers)
+        out, saved = self.block.forward(self.params, index, x, begin, self.seed, draws=draws)
+        diff = out - target
+        self.block.backward(self.params, index, saved, diff / (self.batch * self.block.width), begin, self.grads, workers)
+        return diff.square().mean() / 2
 
     def evaluate(self, x, target):
         """Mean loss of every worker's newest replica on the same samples, without dropout."""
@@ -182,10 +192,13 @@ class Training:
         return loss
 
     def _evaluate(self, x, target):
-        N = len(self.external)
-        begin = torch.arange(0, (N + 1) * len(x), len(x), dtype=torch.int32, device=self.x.device)
-        out, _ = self.block.forward(self.params, self.versions(range(N)), x.to(self.x.device).repeat(N, 1), begin, train=False)
-        return (out.view(N, *target.shape) - target.to(self.x.device)).square().mean((1, 2)) / 2
+        x, target = x.to(self.x.device), target.to(self.x.device)
+        losses = []
+        for run in _runs(range(len(self.external))):
+            begin = torch.arange(0, (len(run) + 1) * len(x), len(x), dtype=torch.int32, device=x.device)
+            out, _ = self.block.forward(self.params, self.versions(run), x.repeat(len(run), 1), begin, train=False)
+            losses.append((out.view(len(run), *target.shape) - target).square().mean((1, 2)) / 2)
+        return losses[0] if len(losses) == 1 else torch.cat(losses)
 
     def close(self):
         self.session.close()
