@@ -9,6 +9,9 @@ written the same way, so `out=` can be the N x d tensor that hop_set_grad_source
 Rows are float32 or bfloat16 with contiguous columns; the distance between rows is free.  Calls enqueue kernels on the current
 stream and return.  What the library refuses raises HopError, what does not fit together ValueError or TypeError; nothing falls
 back to anything else.
+
+Gradients are calls of their own: results carry no history for torch's differentiation.  Where that is enabled, a tensor that requires a
+gradient is refused (call under torch.no_grad(), or with detached tensors); what `out=` and its like are given counts as changed in place.
 """
 import collections
 import ctypes as C
@@ -70,6 +73,12 @@ def load():
 # A kernel of a small call takes less time than its launch (4 us), so what is asked of the arguments is asked in the order that lets plain
 # ones through with few questions, and devices are compared as numbers.
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_changed = torch.autograd.graph.increment_version
+
+
+def _needs_history(name):
+    if torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, which would be lost: results have no history (torch.no_grad() or detach() say that none is wanted)" % name)
 
 
 def _rows(x, name):
@@ -78,6 +87,8 @@ def _rows(x, name):
         dtype = _TYPES[x.dtype]
     except KeyError:
         raise TypeError("%s: float32 or bfloat16 is needed, got %s" % (name, x.dtype)) from None
+    if x.requires_grad:
+        _needs_history(name)
     gpu = x.get_device()
     if gpu < 0:
         raise ValueError("%s: a tensor on the GPU is needed" % name)
@@ -108,6 +119,8 @@ def _ld(t, name, dtype, gpu, rows, cols):
         raise TypeError("%s: %s is needed, got %s" % (name, dtype, t.dtype))
     if t.get_device() != gpu:
         raise ValueError("%s: a tensor on cuda:%d is needed" % (name, gpu))
+    if t.requires_grad:
+        _needs_history(name)
     return _distance(t, name, rows, cols)
 
 
@@ -142,6 +155,8 @@ def _vector(t, name, cols, gpu, M=None):
     shape = t.shape
     if len(shape) != 2 or shape[1] != cols or t.dtype is not torch.float32 or t.get_device() != gpu or (cols > 1 and t.stride(1) != 1):
         raise ValueError("%s: float32 [groups, %d] with contiguous columns on cuda:%d is needed" % (name, cols, gpu))
+    if t.requires_grad:
+        _needs_history(name)
     if M is not None and shape[0] != M:
         raise ValueError("%s: %d rows, other parameters have %d" % (name, shape[0], M))
     return t.data_ptr(), t.stride(0), shape[0]
@@ -153,7 +168,19 @@ def _weights(w, name, gpu):
     if len(shape) != 3 or w.get_device() != gpu or (shape[2] > 1 and stride[2] != 1) or (shape[1] > 1 and stride[1] < shape[2]):
         raise ValueError("%s: [groups, rows, columns] with contiguous columns on cuda:%d is needed, got %s with strides %s"
                          % (name, gpu, list(shape), list(stride)))
+    if w.requires_grad:
+        _needs_history(name)
     return stride[0], max(stride[1], shape[2]), shape
+
+
+def _result(t, x, name, gpu, rows, cols):
+    """(tensor, address, distance) of a result like x."""
+    if t is None:
+        t = x.new_empty((rows, cols))
+        return t, t.data_ptr(), cols
+    ld = _ld(t, name, x.dtype, gpu, rows, cols)
+    _changed(t)
+    return t, t.data_ptr(), ld
 
 
 def _with_scratch(name, like, gpu, *args):
@@ -188,11 +215,8 @@ def product(x, w, row_begin=None, index=None, transposed=False, out=None):
     if w.dtype is not x.dtype or b != k:
         raise ValueError("w: %s [groups, %s] is needed, got %s %s" % (x.dtype, "%d, out" % k if transposed else "out, %d" % k, w.dtype, list(w.shape)))
     idx = _index(index, G, M, "w")
-    if out is None:
-        out, ldy = x.new_empty((rows, a)), a
-    else:
-        ldy = _ld(out, "out", x.dtype, gpu, rows, a)
-    args = _PRODUCT(rows, table, G, dtype, x.data_ptr(), ldx, w.data_ptr(), ldw, step, _address(idx), out.data_ptr(), ldy, k, a,
+    out, y_at, ldy = _result(out, x, "out", gpu, rows, a)
+    args = _PRODUCT(rows, table, G, dtype, x.data_ptr(), ldx, w.data_ptr(), ldw, step, _address(idx), y_at, ldy, k, a,
                     1 if transposed else 0, 0)
     _with_scratch("hop_product", x, gpu, args)
     return out
@@ -214,6 +238,7 @@ def product_grad(dy, x, row_begin=None, out=None, index=None):
         raise ValueError("out: float32 [groups, %d, %d] is needed, got %s %s" % (n, k, out.dtype, list(out.shape)))
     step, lddw, (M, _, _) = _weights(out, "out", gpu)
     idx = _index(index, G, M, "out")
+    _changed(out)
     args = _PRODUCT_GRAD(rows, table, G, dtype, dy.data_ptr(), lddy, x.data_ptr(), ldx, out.data_ptr(), lddw, step, _address(idx), k, n)
     _with_scratch("hop_product_grad", x, gpu, args)
     return out
@@ -223,11 +248,8 @@ def product_grad(dy, x, row_begin=None, out=None, index=None):
 def dropout(x, drop, out=None):
     """x / (1 - p) where the mask of `drop` keeps it, else 0.  The gradient is dropout(dy, drop)."""
     dtype, gpu, ldx, rows, cols = _rows(x, "x")
-    if out is None:
-        out, ldy = x.new_empty((rows, cols)), cols
-    else:
-        ldy = _ld(out, "out", x.dtype, gpu, rows, cols)
-    hop._check((_lib or load()).hop_dropout(dtype, x.data_ptr(), ldx, out.data_ptr(), ldy, rows, cols, _drop(drop), _raw_stream(gpu)), "hop_dropout")
+    out, y_at, ldy = _result(out, x, "out", gpu, rows, cols)
+    hop._check((_lib or load()).hop_dropout(dtype, x.data_ptr(), ldx, y_at, ldy, rows, cols, _drop(drop), _raw_stream(gpu)), "hop_dropout")
     return out
 
 
@@ -253,14 +275,6 @@ def _residual_args(rows, cols, dtype, like, gpu, b, row_begin, index, norm, post
     args = _RESIDUAL(rows, table, G, dtype, cols, b_at, ldb, z_at, ldz, post_at, post_step, pre_at, pre_step, gate_at, gate_step, _address(idx),
                      _at(packed), norm, next_norm, kind, scale, eps, 0)
     return args, (idx, packed), G
-
-
-def _result(t, x, name, gpu, rows, cols):
-    """(tensor, address, distance) of a result like x."""
-    if t is None:
-        t = x.new_empty((rows, cols))
-        return t, t.data_ptr(), cols
-    return t, t.data_ptr(), _ld(t, name, x.dtype, gpu, rows, cols)
 
 
 def residual(x, b, row_begin=None, index=None, norm="rms", post=None, gate=None, gate_logits=None, scale=1.0, drop=None, next_norm=None, pre=None, eps=1e-5,
@@ -339,6 +353,8 @@ def residual_grad(dy, dh, y, b, row_begin=None, index=None, norm="rms", post=Non
                     raise ValueError("grad_index without %s" % name)
                 grads[i] = like.new_empty((G, cols), dtype=torch.float32)
             at, step, M = _vector(grads[i], name, cols, gpu, M)
+            if grads[i] is not None:
+                _changed(grads[i])
             packed += (at, step)
     idx = None if M is None else _index(grad_index, G, M, "dpost, dpre, dgate")
     out = _GRADS(dy_at, lddy, dh_at, lddh, y_at, ldy, dx_at, lddx, db_at, lddb, dz_at, lddz, *packed, _address(idx))
