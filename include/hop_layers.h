@@ -29,7 +29,7 @@
  *  - Calls enqueue kernels on `stream` and return (no allocation, no copy, no wait); they can be captured into a HIP graph.
  *    `scratch` is device memory, 16-byte aligned, of at least the bytes that the matching *_scratch_bytes call names (which may
  *    be 0); it is free again when the call's kernels have run.  Results are the same bits on every call with the same arguments.
- *  - Sizes: rows below 2^30 - 65536, products' columns up to 2^21, dropout's up to 2^29; anything else, like every null pointer, misaligned
+ *  - Sizes: rows below 2^30 - 65536, products' columns up to 2^21 and results up to 2^40 elements, dropout's up to 2^29; anything else, like every null pointer, misaligned
  *    address, distance below the columns, unknown enum value and index below zero, is HOP_ERR_INVALID_ARG and nothing is launched; too
  *    little scratch is HOP_ERR_ARENA_TOO_SMALL.
  *  - No rows (rows = 0): nothing is written except the gradients of parameters, which are zero.

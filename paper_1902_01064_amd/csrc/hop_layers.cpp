@@ -15,7 +15,8 @@ namespace {
 constexpr uint64_t STREAM_DROPOUT = 8;         // beside hoprng's streams
 constexpr int64_t kMostRows = (1 << 30) - 65536;
 constexpr int64_t kMostDropCols = 1 << 29;     // a place in a row is a 32-bit number of bytes
-constexpr int64_t kMostCols = 1 << 21;         // a grid has room for 65535 tiles
+constexpr int64_t kMostCols = 1 << 21;         // a tile's lines, up to 2^20 elements apart, end within the 31 bits of a buffer's places
+constexpr int64_t kMostResults = (int64_t)1 << 40;             // elements of a product's result: tiles are counted in 31 bits
 
 int hip_fail(hipError_t e, const char* what) {
     std::fprintf(stderr, "libhop: %s: %s\n", what, hipGetErrorString(e));
@@ -79,6 +80,7 @@ HopMask mask_of(const hop_drop* d) {
 
 bool product_ok(const hop_product_args* a) {
     if (!a || !groups_ok(a->groups, a->w_index != nullptr) || a->in < 1 || a->in > kMostCols || a->out < 1 || a->out > kMostCols) return false;
+    if (a->groups.rows > kMostResults / a->out) return false;
     const size_t e = type_bytes(a->groups.dtype);
     return matrix_ok(a->w, a->ldw, a->transposed ? a->out : a->in, e) && vectors_ok(nullptr, a->w_stride) && index_ok(a->w_index, a->groups.G) &&
            (a->groups.rows == 0 || (matrix_ok(a->x, a->ldx, a->in, e) && matrix_ok(a->y, a->ldy, a->out, e)));
@@ -95,6 +97,7 @@ HopProductTask product_task(const hop_product_args* a) {
 
 bool product_grad_ok(const hop_product_grad_args* a) {
     if (!a || !groups_ok(a->groups, a->dw_index != nullptr) || a->in < 1 || a->in > kMostCols || a->out < 1 || a->out > kMostCols) return false;
+    if (a->groups.G > kMostResults / a->out / a->in) return false;
     const size_t e = type_bytes(a->groups.dtype);
     return matrix_ok(a->dw, a->lddw, a->in, 4) && vectors_ok(nullptr, a->dw_stride) && index_ok(a->dw_index, a->groups.G) &&
            distinct(a->dw_index, a->groups.G) && apart(a->dw_index, a->groups.G, a->dw_stride, a->out, a->lddw, a->in) &&

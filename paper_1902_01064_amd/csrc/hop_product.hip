@@ -338,10 +338,11 @@ __device__ __forceinline__ void staged_product(const T* p, int64_t ldp, int np, 
 
 // Which tile a workgroup takes.  Workgroups are dealt to the 8 XCDs in turn; an XCD takes runs of up to 32 tiles (a workgroup for each of its CUs),
 // kBand pieces of rows by 8 columns of tiles, so that both operands' tiles are found in its L2 again, and the runs go round the XCDs, so
-// that each gets its share of whole and of short pieces.
+// that each gets its share of whole and of short pieces.  `most` is the number of workgroups for all tiles that there can be: a launch may hold
+// a part of them only, from workgroup `first` on.
 constexpr int kBand = 4, kRun = 32;
-__device__ __forceinline__ bool place_tile(int b, int pieces, int columns, int* piece, int* column) {
-    pieces = min(pieces, (int)gridDim.x / columns);         // what a proper row table has at most
+__device__ __forceinline__ bool place_tile(int b, int most, int pieces, int columns, int* piece, int* column) {
+    pieces = min(pieces, most / columns);                   // what a proper row table has at most
     const int total = pieces * columns, rounds = (total + 8 * kRun - 1) / (8 * kRun);
     if (!total) return false;
     const int run = (total + 8 * rounds - 1) / (8 * rounds), turn = b / 8;      // as many runs for every XCD
@@ -356,14 +357,14 @@ __device__ __forceinline__ bool place_tile(int b, int pieces, int columns, int* 
 
 // PART: the contraction is cut in gridDim.y parts, whose sums go to partial[part][row][column] in 32 bits.
 template <typename T, bool TRANSPOSED, bool PART, bool FED, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void product_staged_kernel(HopProductTask t, int columns, HopIndex index) {
+__global__ __launch_bounds__(WM* WN * 64) void product_staged_kernel(HopProductTask t, int columns, int first, int most, HopIndex index) {
     constexpr int shift = __builtin_ctz(BM), kK = kStepBytes / sizeof(T);
     int piece, column, g, r0, r1;
     if constexpr (BM >= 256) {
         const WholePieces all = count_whole(t.rows, shift);
-        if (!place_tile(blockIdx.x, all.whole + all.rest, columns, &piece, &column) || !find_whole(t.rows, shift, all, piece, &g, &r0, &r1)) return;
+        if (!place_tile(first + blockIdx.x, most, all.whole + all.rest, columns, &piece, &column) || !find_whole(t.rows, shift, all, piece, &g, &r0, &r1)) return;
     } else {                    // a group's pieces together: they share its weights
-        if (!place_tile(blockIdx.x, count_pieces(t.rows, shift), columns, &piece, &column) || !find_piece(t.rows, shift, piece, &g, &r0, &r1)) return;
+        if (!place_tile(first + blockIdx.x, most, count_pieces(t.rows, shift), columns, &piece, &column) || !find_piece(t.rows, shift, piece, &g, &r0, &r1)) return;
     }
     const int64_t n0 = (int64_t)column * BN;
     const int at = t.indexed ? index.at[g] : g;
@@ -381,10 +382,10 @@ __global__ __launch_bounds__(WM* WN * 64) void product_staged_kernel(HopProductT
 
 // PART: the group's rows are cut in gridDim.y parts, whose sums go to partial[part][g][out][in].
 template <typename T, bool PART, bool FED, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void product_grad_staged_kernel(HopProductGradTask t, int tiles_out, int tiles_in, HopIndex index) {
+__global__ __launch_bounds__(WM* WN * 64) void product_grad_staged_kernel(HopProductGradTask t, int tiles_out, int tiles_in, int first, HopIndex index) {
     constexpr int kK = kStepBytes / sizeof(T);
     // Groups differ in length, so every group's tiles are dealt to all XCDs, a run of them to each (operands' tiles are shared in its L2).
-    const int tiles = tiles_out * tiles_in, each_xcd = (tiles + 7) / 8, x = blockIdx.x % 8, turn = blockIdx.x / 8;
+    const int tiles = tiles_out * tiles_in, each_xcd = (tiles + 7) / 8, x = blockIdx.x % 8, turn = (first + (int)blockIdx.x) / 8;
     const int g = turn / each_xcd, tile = x * each_xcd + turn % each_xcd;
     if (tile >= tiles) return;
     const int row = tile / tiles_in, column = tile % tiles_in;
@@ -500,18 +501,25 @@ int64_t pieces_of(const HopRows& rows, int step) { return (rows.rows + (int64_t)
 // Workgroups that place_tile needs to see them all.
 int64_t tile_grid(int64_t tiles) { return 8 * ((tiles + 7) / 8 + (tiles + 8 * kRun - 1) / (8 * kRun)); }
 
+// A launch holds fewer than 2^32 threads.  More workgroups than these go in several (parts of a multiple of 8, so that XCDs get what they would).
+constexpr int64_t kMostBlocks = 1 << 22;
+template <typename F>
+void in_launches(int64_t blocks, F launch) {
+    for (int64_t first = 0; first < blocks; first += kMostBlocks) launch((int)first, (unsigned)std::min(kMostBlocks, blocks - first));
+}
+
 template <typename T, bool FED, int BM, int BN, int WM, int WN>
 void launch_staged(const HopProductTask& t, int transposed, int parts, const HopIndex& index, hipStream_t st) {
-    const int64_t columns = (t.out + BN - 1) / BN, tiles = pieces_of(t.rows, BM) * columns;
-    const dim3 grid((unsigned)tile_grid(tiles), (unsigned)parts), block(WM * WN * 64);
-    if (parts > 1) {
-        if (transposed) product_staged_kernel<T, true, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
-        else product_staged_kernel<T, false, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
+    const int64_t columns = (t.out + BN - 1) / BN, most = tile_grid(pieces_of(t.rows, BM) * columns);
+    in_launches(most, [&](int first, unsigned blocks) {
+        const dim3 grid(blocks, (unsigned)parts), block(WM * WN * 64);
+        if (parts > 1 && transposed) product_staged_kernel<T, true, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, first, (int)most, index);
+        else if (parts > 1) product_staged_kernel<T, false, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, first, (int)most, index);
+        else if (transposed) product_staged_kernel<T, true, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, first, (int)most, index);
+        else product_staged_kernel<T, false, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, first, (int)most, index);
+    });
+    if (parts > 1)
         product_join_kernel<T><<<join_blocks(t.rows.rows, t.out), 256, 0, st>>>(t.partial, parts, t.rows.rows, t.out, (T*)t.y, t.ldy, 0, 0, 0, index);
-    } else {
-        if (transposed) product_staged_kernel<T, true, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
-        else product_staged_kernel<T, false, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)columns, index);
-    }
 }
 template <typename T, bool FED>
 void launch_tile(const HopProductTask& t, int transposed, const HopProductPlan& p, const HopIndex& index, hipStream_t st) {
@@ -532,13 +540,14 @@ void launch_few(const HopProductTask& t, int tile, const HopIndex& index, hipStr
 template <typename T, bool FED, int BM, int BN, int WM, int WN>
 void launch_grad_staged(const HopProductGradTask& t, int parts, const HopIndex& index, hipStream_t st) {
     const int64_t out = (t.out + BM - 1) / BM, in = (t.in + BN - 1) / BN;
-    const dim3 grid((unsigned)(t.rows.G * ((out * in + 7) / 8 * 8)), (unsigned)parts);
+    in_launches(t.rows.G * ((out * in + 7) / 8 * 8), [&](int first, unsigned blocks) {
+        const dim3 grid(blocks, (unsigned)parts), block(WM * WN * 64);
+        if (parts > 1) product_grad_staged_kernel<T, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)out, (int)in, first, index);
+        else product_grad_staged_kernel<T, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)out, (int)in, first, index);
+    });
     if (parts > 1) {
-        product_grad_staged_kernel<T, true, FED, BM, BN, WM, WN><<<grid, WM * WN * 64, 0, st>>>(t, (int)out, (int)in, index);
         const int64_t rows = (int64_t)t.rows.G * t.out;
         product_join_kernel<float><<<join_blocks(rows, t.in), 256, 0, st>>>(t.partial, parts, rows, t.in, t.dw, t.lddw, t.out, t.dw_stride, t.indexed, index);
-    } else {
-        product_grad_staged_kernel<T, false, FED, BM, BN, WM, WN><<<grid, WM * WN * 64, 0, st>>>(t, (int)out, (int)in, index);
     }
 }
 
@@ -585,7 +594,6 @@ HopProductPlan hopl_product_plan(const HopProductTask& t, int dtype, int transpo
         TileCost c = dtype == HOP_BF16 ? kTilesBf16[i] : kTilesF32[i];
         if (!fed) c.full *= 1.2, c.least *= 1.4;       // through registers (4096 x 4096 x 4095 in fp32: 1166 us, 994 when fed)
         if (dtype == HOP_F32 && transposed && i == 2) c.full *= 1.15;          // its reads of single words from LDS (4096^3: 1157 us, 1000 the other way)
-        if (pieces_of(t.rows, c.bm) * ((t.out + c.bn - 1) / c.bn) > 1 << 22) continue;
         const double per = R <= c.bm / 2 ? 1 : R / c.bm + 0.5, fill = std::min(1.0, (R + c.grain / 2) / (per * c.bm));
         const double units = G * per * std::ceil(out / c.bn), steps = std::ceil(in * e / kStepBytes);
         for (int parts = 1; parts <= 8; parts *= 2) {
@@ -619,7 +627,6 @@ HopProductPlan hopl_product_grad_plan(const HopProductGradTask& t, int dtype) {
     for (int i = fed || dtype != HOP_BF16 ? 0 : 1; i < (dtype == HOP_BF16 ? 3 : 2); ++i) {
         const TileCost& c = dtype == HOP_BF16 ? kGradTilesBf16[i] : kGradTilesF32[i];
         const double units = G * std::ceil((double)t.out / c.bm) * std::ceil((double)t.in / c.bn), steps = std::ceil(R * e / kStepBytes);
-        if (units > 1 << 22) continue;
         for (int parts = 1; parts <= 8; parts *= 2) {
             if (parts > 1 && (steps < 2 * parts || units * parts > 10 * kCus)) break;
             double us = kLaunch + 1.5 * (2 - i) + written / kHbm + steps_time(c, units * parts, std::ceil(steps / parts), 1.0, false);
