@@ -537,13 +537,20 @@ void launch_few(const HopProductTask& t, int tile, const HopIndex& index, hipStr
     else product_few_kernel<T, 2, 16><<<grid, 1024, 0, st>>>(t, index);
 }
 
+// Gradients in 32 bits on 128 x 128 tiles are not cut in parts: 64 x 64 tiles take 0.99 of the time a step and have the grain of four parts with
+// nothing to join, so the estimate never came out that way (1.6 million sizes).
+template <typename T, int BM>
+constexpr bool kInParts = sizeof(T) == 2 || BM < 128;
+
 template <typename T, bool FED, int BM, int BN, int WM, int WN>
 void launch_grad_staged(const HopProductGradTask& t, int parts, const HopIndex& index, hipStream_t st) {
     const int64_t out = (t.out + BM - 1) / BM, in = (t.in + BN - 1) / BN;
     in_launches(t.rows.G * ((out * in + 7) / 8 * 8), [&](int first, unsigned blocks) {
         const dim3 grid(blocks, (unsigned)parts), block(WM * WN * 64);
-        if (parts > 1) product_grad_staged_kernel<T, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)out, (int)in, first, index);
-        else product_grad_staged_kernel<T, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)out, (int)in, first, index);
+        if constexpr (kInParts<T, BM>) {
+            if (parts > 1) return product_grad_staged_kernel<T, true, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)out, (int)in, first, index);
+        }
+        product_grad_staged_kernel<T, false, FED, BM, BN, WM, WN><<<grid, block, 0, st>>>(t, (int)out, (int)in, first, index);
     });
     if (parts > 1) {
         const int64_t rows = (int64_t)t.rows.G * t.out;
@@ -626,9 +633,10 @@ HopProductPlan hopl_product_grad_plan(const HopProductGradTask& t, int dtype) {
     double least = 1e300;
     for (int i = fed || dtype != HOP_BF16 ? 0 : 1; i < (dtype == HOP_BF16 ? 3 : 2); ++i) {
         const TileCost& c = dtype == HOP_BF16 ? kGradTilesBf16[i] : kGradTilesF32[i];
+        const bool cut = dtype == HOP_BF16 || i > 0;             // kInParts
         const double units = G * std::ceil((double)t.out / c.bm) * std::ceil((double)t.in / c.bn), steps = std::ceil(R * e / kStepBytes);
         for (int parts = 1; parts <= 8; parts *= 2) {
-            if (parts > 1 && (steps < 2 * parts || units * parts > 10 * kCus)) break;
+            if (parts > 1 && (!cut || steps < 2 * parts || units * parts > 10 * kCus)) break;
             double us = kLaunch + 1.5 * (2 - i) + written / kHbm + steps_time(c, units * parts, std::ceil(steps / parts), 1.0, false);
             if (parts > 1) us += 3 + 2 * parts * written / kHbm;
             if (us < least) least = us, best = {fed ? HOPL_FED : HOPL_ANY, parts, i};
