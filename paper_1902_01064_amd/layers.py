@@ -287,6 +287,8 @@ def residual(x, b, row_begin=None, index=None, norm="rms", post=None, gate=None,
     if b is None:
         raise ValueError("b: a matrix is needed (norm() is a norm by itself)")
     args, keep, _ = _residual_args(rows, cols, dtype, x.dtype, gpu, b, row_begin, index, norm, post, gate, gate_logits, scale, drop, next_norm, pre, eps)
+    if next_norm is None and out_next is not None:
+        raise ValueError("out_next without next_norm")
     y, y_at, ldy = _result(out, x, "out", gpu, rows, cols)
     h, h_at, ldh = (None, None, 0) if next_norm is None else _result(out_next, x, "out_next", gpu, rows, cols)
     hop._check((_lib or load()).hop_residual(args, x.data_ptr(), ldx, y_at, ldy, h_at, ldh, _raw_stream(gpu)), "hop_residual")
