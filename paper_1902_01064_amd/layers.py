@@ -196,7 +196,12 @@ def _with_scratch(name, like, gpu, *args):
 
 
 def _drop(drop):
-    return None if drop is None else _DROP(drop.seed & ((1 << 64) - 1), drop.first_row, drop.worker, drop.iter, drop.site, drop.p)
+    if drop is None:
+        return None
+    try:
+        return _DROP(drop.seed & ((1 << 64) - 1), drop.first_row, drop.worker, drop.iter, drop.site, drop.p)
+    except struct.error as e:
+        raise ValueError("%s: %s" % (drop, e)) from None
 
 
 def _at(packed):
@@ -272,8 +277,11 @@ def _residual_args(rows, cols, dtype, like, gpu, b, row_begin, index, norm, post
         norm, next_norm = _NORMS[norm], _NORMS[next_norm]
     except (KeyError, TypeError):
         raise ValueError("norm: None, 'rms' or 'centred'") from None
-    args = _RESIDUAL(rows, table, G, dtype, cols, b_at, ldb, z_at, ldz, post_at, post_step, pre_at, pre_step, gate_at, gate_step, _address(idx),
-                     _at(packed), norm, next_norm, kind, scale, eps, 0)
+    try:
+        args = _RESIDUAL(rows, table, G, dtype, cols, b_at, ldb, z_at, ldz, post_at, post_step, pre_at, pre_step, gate_at, gate_step, _address(idx),
+                         _at(packed), norm, next_norm, kind, scale, eps, 0)
+    except struct.error as e:
+        raise ValueError("scale %s, eps %s: %s" % (scale, eps, e)) from None
     return args, (idx, packed), G
 
 
