@@ -623,33 +623,35 @@ int shift_for(int64_t rows, int64_t pieces) {
 
 int64_t pieces_of(int64_t rows, int G, int shift) { return (rows >> shift) + (G < rows ? G : rows); }
 
-template <typename T, int NT, int V, bool EVEN>
-void launch(const HopResidualTask& t, const HopIndex& index, int64_t pieces, bool grad, hipStream_t st) {
+template <typename T, int NT, int V, bool EVEN, bool GRAD>
+void launch(const HopResidualTask& t, const HopIndex& index, int64_t pieces, hipStream_t st) {
     const dim3 grid((unsigned)pieces);
-    if (grad && t.z) residual_grad_kernel<T, NT, V, EVEN, true><<<grid, NT, 0, st>>>(t, index);
-    else if (grad) residual_grad_kernel<T, NT, V, EVEN, false><<<grid, NT, 0, st>>>(t, index);
-    else residual_kernel<T, NT, V, EVEN><<<grid, NT, 0, st>>>(t, index);
+    if constexpr (!GRAD) residual_kernel<T, NT, V, EVEN><<<grid, NT, 0, st>>>(t, index);
+    else if (t.z) residual_grad_kernel<T, NT, V, EVEN, true><<<grid, NT, 0, st>>>(t, index);
+    else residual_grad_kernel<T, NT, V, EVEN, false><<<grid, NT, 0, st>>>(t, index);
 }
-template <typename T, bool EVEN>
-void launch(const HopResidualTask& t, const HopIndex& index, int64_t pieces, bool grad, hipStream_t st) {
-    if (t.cols <= 512) launch<T, 64, 1, EVEN>(t, index, pieces, grad, st);
-    else if (t.cols <= 1024) launch<T, 128, 1, EVEN>(t, index, pieces, grad, st);
-    else if (t.cols <= 2048) launch<T, 256, 1, EVEN>(t, index, pieces, grad, st);
-    else if (t.cols <= 4096) launch<T, 512, 1, EVEN>(t, index, pieces, grad, st);
-    else if (t.cols <= 6144) launch<T, 768, 1, EVEN>(t, index, pieces, grad, st);
-    else if (t.cols <= 8192 && !(grad && sizeof(T) == 4)) launch<T, 1024, 1, EVEN>(t, index, pieces, grad, st);
-    else if (t.cols <= 8192) launch<T, 512, 2, EVEN>(t, index, pieces, grad, st);
-    else if (t.cols <= 16384) launch<T, 1024, 2, EVEN>(t, index, pieces, grad, st);
-    else launch<T, 1024, 4, EVEN>(t, index, pieces, grad, st);
+template <typename T, bool EVEN, bool GRAD>
+void launch(const HopResidualTask& t, const HopIndex& index, int64_t pieces, hipStream_t st) {
+    // 1024 threads leave a gradient in 32 bits short of registers (4096 x 8192 with a gate for every element: 265 us, 234 with 512 threads of twice
+    // eight columns; without gate 180 both ways, 7001 columns 199 and 210)
+    constexpr int kTwice = GRAD && sizeof(T) == 4 ? 2 : 1;
+    if (t.cols <= 512) launch<T, 64, 1, EVEN, GRAD>(t, index, pieces, st);
+    else if (t.cols <= 1024) launch<T, 128, 1, EVEN, GRAD>(t, index, pieces, st);
+    else if (t.cols <= 2048) launch<T, 256, 1, EVEN, GRAD>(t, index, pieces, st);
+    else if (t.cols <= 4096) launch<T, 512, 1, EVEN, GRAD>(t, index, pieces, st);
+    else if (t.cols <= 6144) launch<T, 768, 1, EVEN, GRAD>(t, index, pieces, st);
+    else if (t.cols <= 8192) launch<T, 1024 / kTwice, kTwice, EVEN, GRAD>(t, index, pieces, st);
+    else if (t.cols <= 16384) launch<T, 1024, 2, EVEN, GRAD>(t, index, pieces, st);
+    else launch<T, 1024, 4, EVEN, GRAD>(t, index, pieces, st);
 }
-template <typename T>
-void launch(const HopResidualTask& t, const HopIndex& index, int64_t pieces, bool grad, hipStream_t st) {
+template <typename T, bool GRAD>
+void launch(const HopResidualTask& t, const HopIndex& index, int64_t pieces, hipStream_t st) {
     // buffer accesses want addresses that are multiples of four
     auto even = [](const void* p, int64_t ld) { return ((uintptr_t)p & 3u) == 0 && (!p || ld * (int64_t)sizeof(T) % 4 == 0); };
     const bool all = t.cols % 8 == 0 && even(t.x, t.ldx) && even(t.b, t.ldb) && even(t.z, t.ldz) && even(t.y, t.ldy) && even(t.h, t.ldh) &&
                      even(t.dy, t.lddy) && even(t.dh, t.lddh) && even(t.dx, t.lddx) && even(t.db, t.lddb) && even(t.dz, t.lddz);
-    if (all) launch<T, true>(t, index, pieces, grad, st);
-    else launch<T, false>(t, index, pieces, grad, st);
+    if (all) launch<T, true, GRAD>(t, index, pieces, st);
+    else launch<T, false, GRAD>(t, index, pieces, st);
 }
 
 }  // namespace
@@ -670,8 +672,8 @@ int hopl_residual(HopResidualTask t, int dtype, const HopIndex& index, void* str
     // 256 113, 16384 151)
     t.shift = shift_for(t.rows.rows, t.cols <= 4096 ? 256 * 4096 / threads_for(t.cols) : 256);
     const int64_t pieces = pieces_of(t.rows.rows, t.rows.G, t.shift);
-    if (dtype == HOP_BF16) launch<bf16>(t, index, pieces, false, (hipStream_t)stream);
-    else launch<float>(t, index, pieces, false, (hipStream_t)stream);
+    if (dtype == HOP_BF16) launch<bf16, false>(t, index, pieces, (hipStream_t)stream);
+    else launch<float, false>(t, index, pieces, (hipStream_t)stream);
     return (int)hipGetLastError();
 }
 
@@ -687,8 +689,8 @@ int hopl_residual_grad(HopResidualTask t, int dtype, const HopIndex& index, cons
     t.shift = hopl_grad_shift(t.rows.rows, t.cols);
     const int64_t chunks = pieces_of(t.rows.rows, t.rows.G, t.shift);
     if (chunks > 0) {
-        if (dtype == HOP_BF16) launch<bf16>(t, index, chunks, true, st);
-        else launch<float>(t, index, chunks, true, st);
+        if (dtype == HOP_BF16) launch<bf16, true>(t, index, chunks, st);
+        else launch<float, true>(t, index, chunks, st);
     }
     if (t.dpost || t.dpre || t.dgate) {
         const dim3 grid((unsigned)((t.cols + 63) / 64), (unsigned)t.rows.G, 3);
