@@ -45,7 +45,7 @@ extern "C" {
 
 #define HOP_MAX_GROUPS 4096        /* most groups of a call */
 #define HOP_MAX_INDEXED 256        /* most groups of a call with an index list */
-#define HOP_MAX_NORM_COLS 32768    /* widest row of hop_residual; up to 16384 are what it is fast for */
+#define HOP_MAX_NORM_COLS 32768    /* widest row of hop_residual; up to 8192 are what it is fast for */
 
 enum { HOP_F32 = 0, HOP_BF16 = 1 };
 /* none; x / sqrt(mean x^2 + eps); (x - mean x) / sqrt(var x + eps) */

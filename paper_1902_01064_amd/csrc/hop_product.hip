@@ -431,10 +431,12 @@ inline unsigned join_blocks(int64_t rows, int cols) {
 // ---- few rows -----------------------------------------------------------------------
 // 16 FM rows by 16 columns: the weights are read once, straight into the registers that the matrix unit takes them from (a lane holds 32
 // consecutive bytes of its line, four lanes a cache line), by four wavefronts that take turns along the contraction and join their
-// sums in LDS.  Bound by reading the weights; a tile's share of them is a few KB, so that small layers have workgroups for every CU.
+// sums in LDS.  Bound by reading the weights; a tile's share of them is a few KB, so that small layers have workgroups for every CU.  Of a pass's
+// 16 to 24 loads a wavefront, 16 rows in bf16 have eight on their way as the compiler orders them, 32 rows five to seven (over 16 wavefronts four),
+// fp32 four.
 template <typename T, int FM, int kFewWaves>
 __global__ __launch_bounds__(kFewWaves * 64) void product_few_kernel(HopProductTask t, HopIndex index) {
-    constexpr int kChunk = 16 / sizeof(T), kK = 8 * kChunk, kUnroll = 4;      // elements of a load, of a turn; turns in flight
+    constexpr int kChunk = 16 / sizeof(T), kK = 8 * kChunk, kUnroll = 4;      // elements of a load, of a turn; turns a pass of the loop
     __shared__ f32x4 s[kFewWaves][FM][64];
     int g, r0, r1;
     if (!find_piece(t.rows, 4 + (FM >> 1), blockIdx.y, &g, &r0, &r1)) return;
@@ -562,16 +564,17 @@ void launch_grad_staged(const HopProductGradTask& t, int parts, const HopIndex& 
 // Tiles and parts are chosen by an estimate of each way's time from the sizes; how the rows fall to the groups is not known here, so
 // groups are taken for equal.  The constants are measured (MI355X, us): `full`, a step of 128 bytes of the contraction on a CU that
 // has enough workgroups (bf16 256 x 256: 8192^3 in 884 us; fp32 128 x 128: 4096^3 in 978); `least`, of a workgroup that has the CU to itself, bound
-// by the loads' latency; `own`, what a workgroup costs beside its steps; `beside`, workgroups that a CU holds.
+// by the loads' latency; `beside`, workgroups that a CU holds; `own`, what a workgroup costs beside its steps (told apart for gradients only).
 struct TileCost {
     int bm, bn, grain;             // rows and columns; rows that a short piece is rounded up to
-    double full, least, own;
+    double full, least;
     int beside;
+    double own = 0.0;
 };
-constexpr TileCost kTilesBf16[4] = {{256, 256, 64, 1.75, 0.85, 0.0, 1}, {128, 128, 64, 0.49, 0.55, 0.0, 2}, {64, 64, 64, 0.24, 0.45, 0.0, 5}, {32, 128, 32, 0.28, 0.46, 0.0, 4}};
-constexpr TileCost kTilesF32[4] = {{0, 0, 0, 0, 0, 0, 0}, {128, 128, 32, 1.91, 0.75, 0.0, 2}, {64, 64, 32, 0.49, 0.62, 0.0, 5}, {32, 128, 16, 0.50, 0.60, 0.0, 4}};
-constexpr TileCost kGradTilesBf16[3] = {{256, 256, 64, 1.75, 1.1, 0.0, 1}, {128, 128, 64, 0.60, 0.67, 0.5, 2}, {64, 64, 64, 0.35, 0.45, 0.3, 4}};
-constexpr TileCost kGradTilesF32[2] = {{128, 128, 32, 1.93, 2.1, 0.0, 2}, {64, 64, 32, 0.48, 0.65, 0.2, 4}};
+constexpr TileCost kTilesBf16[4] = {{256, 256, 64, 1.75, 0.85, 1}, {128, 128, 64, 0.49, 0.55, 2}, {64, 64, 64, 0.24, 0.45, 5}, {32, 128, 32, 0.28, 0.46, 4}};
+constexpr TileCost kTilesF32[4] = {{0, 0, 0, 0, 0, 0}, {128, 128, 32, 1.91, 0.75, 2}, {64, 64, 32, 0.49, 0.62, 5}, {32, 128, 16, 0.50, 0.60, 4}};
+constexpr TileCost kGradTilesBf16[3] = {{256, 256, 64, 1.75, 1.1, 1}, {128, 128, 64, 0.60, 0.67, 2, 0.5}, {64, 64, 64, 0.35, 0.45, 4, 0.3}};
+constexpr TileCost kGradTilesF32[2] = {{128, 128, 32, 1.93, 2.1, 2}, {64, 64, 32, 0.48, 0.65, 4, 0.2}};
 constexpr double kCus = 256, kHbm = 5.2e6, kJoin = 6e6, kLaunch = 4;       // bytes a us; us
 
 // Steps of `units` workgroups; `fill`: the part of a tile that is not padding; `far`: the weights are too many for the caches, which the
@@ -610,8 +613,8 @@ HopProductPlan hopl_product_plan(const HopProductTask& t, int dtype, int transpo
             consider(us, {fed ? HOPL_FED : HOPL_ANY, parts, i});
         }
     }
-    // Few rows: a turn of all wavefronts takes 1.25 us when nothing else is in its way; with 32 rows the weights come at 3 TB/s (64 rows of
-    // 4096 x 4096 in bf16 26 us), with 16 at 5 (33 us).  Sixteen wavefronts where there are too few workgroups for four of them each (1 row, 8192 x 1024:
+    // Few rows: a turn of all wavefronts takes 1.25 us when nothing else is in its way; the kernel of 32 rows, with fewer loads on their way, reads
+    // the weights at 3 TB/s (64 rows of 4096 x 4096 in bf16 26 us), that of 16 at 5 (33 us).  Sixteen wavefronts where there are too few workgroups for four of them each (1 row, 8192 x 1024:
     // 14.2 -> 12.7 us; 8 rows over 8 groups of 1024 x 1024 6.6 -> 9.6).
     if (fed && !transposed && R <= 128 && T * in * out < 1e12) {
         for (int wide = 0; wide < 2; ++wide) {

@@ -4,7 +4,8 @@
 //   e = dy + next_norm'(dh pre; y), f = scale dropout(e), q = f gate, db = norm'(q post; b), norm'(a; v) = r (a - [mean a] - n mean(a n))
 //
 // A row is read once, stays in registers through its statistics (eight consecutive columns a thread), and is written once; the mask is worked
-// out again wherever it is needed.  About 39 vector instructions an element forwards and 54 back, the generator's among them, so instruction issue comes
+// out again wherever it is needed.  That holds up to 8192 columns: wider rows' kernels spill 50 to 200 registers a thread, over 16384 up to 1700.  The next
+// row is loaded ahead where rows are whole pieces of eight columns; elsewhere the loads wait for each other (see columns8).  About 39 vector instructions an element forwards and 54 back, the generator's among them, so instruction issue comes
 // close behind the bytes: 16384 x 4096 in bf16 with dropout 103 us forwards (5.2 TB/s of the 537 MB), 170 back (4.7 TB/s of 805); dropout of
 // 8192 x 8192 in bf16 48 us (5.6 TB/s).  With few rows the chain of a row - loads, two to four sums over the workgroup - bounds it: 8 rows of 4096 5.6 us.
 #include <type_traits>
@@ -21,7 +22,8 @@ template <typename T>
 __device__ __forceinline__ f32x8 wide(raw_of<T> v) { return __builtin_convertvector(v, f32x8); }
 // Eight columns of a row from byte `at` on, as they are; n <= 8 of them exist (n <= 0: none), the rest are zero.  At the end of a row that is no
 // multiple of eight, the row's last eight are loaded and moved down: single loads there held a register pair each, or waited
-// for each other.  `at` is 32 bits wide and `line` the same for all threads, so an address takes one register.
+// for each other.  `at` is 32 bits wide and `line` the same for all threads, so an address takes one register.  Whether to move down is a
+// branch on what was loaded, so a load's wait stands right behind it.
 __device__ __forceinline__ u32x4 moved_down(u32x4 v, int by) {          // by elements of 16 bits
     if (by & 4) v = u32x4{v[2], v[3], 0, 0};
     if (by & 2) v = u32x4{v[1], v[2], v[3], 0};
@@ -250,13 +252,14 @@ __device__ __forceinline__ f32x8 logistic(f32x8 z) {
     return z;
 }
 
-// The vectors of a group that a workgroup needs for all its rows wait in LDS, each thread's own columns (so there is no barrier), while that
-// has room for them: 12 bytes a column, rows of up to 8192.  In registers they would take the place of rows under way.
+// The vectors of a group that a workgroup needs for all its rows wait in LDS, each thread's own columns (so there is no barrier; in registers they
+// would take the place of rows under way): two of them forwards, 8 bytes a column, three back, 12.  Kept for rows of up to 8192 columns, which are those
+// whose next row is loaded ahead: beyond, 12 bytes a column are more than the LDS, and the registers do not hold even the one row (see launch).
 template <int NT, int V>
 struct Vectors {
     static constexpr bool kKept = NT * V <= 1024;
     f32x4 (*kept)[2 * V][kKept ? NT : 1];
-    __device__ __forceinline__ void put(int w, int i, f32x8 v) {
+    __device__ __forceinline__ void put(int w, int i, f32x8 v) const {
         kept[w][2 * i][threadIdx.x] = f32x4{v[0], v[1], v[2], v[3]};
         kept[w][2 * i + 1][threadIdx.x] = f32x4{v[4], v[5], v[6], v[7]};
     }
@@ -294,8 +297,8 @@ __global__ __launch_bounds__(NT) void residual_kernel(HopResidualTask t, HopInde
     if constexpr (Vec::kKept) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            Vec{kept}.put(0, i, global_branch(i));
-            Vec{kept}.put(1, i, global(t.pre, t.pre_stride, i));
+            vec.put(0, i, global_branch(i));
+            vec.put(1, i, global(t.pre, t.pre_stride, i));
         }
     }
     typedef Matrix<T, EVEN> M;
@@ -309,7 +312,7 @@ __global__ __launch_bounds__(NT) void residual_kernel(HopResidualTask t, HopInde
             nz[i] = mz.load(r, col[i], n[i]);
         }
     };
-    constexpr bool kAhead = Vec::kKept;
+    constexpr bool kAhead = NT * V <= 1024;
     if (kAhead) fetch(r0);
     for (int r = r0; r < r1; ++r) {
         if (!kAhead) fetch(r);
@@ -425,16 +428,16 @@ __device__ __forceinline__ void through_norm(f32x8 (&a)[V], const f32x8 (&nv)[V]
         for (int j = 0; j < 8; ++j) a[i][j] = fmaf(nv[i][j], sn, a[i][j] * r);
 }
 
-// As in the forward pass; the parameters' gradients are summed over the piece's rows in registers and leave once a piece, the group's
-// vectors wait in LDS (each thread's own columns: no barrier; with them in registers, 512 threads would fit a CU once, not twice).
-// Z: the gate is a tensor.
+// As in the forward pass; the parameters' gradients are summed over the piece's rows in registers and leave once a piece (with the group's
+// vectors in registers too, 512 threads would fit a CU once, not twice).  Z: the gate is a tensor.
 template <typename T, int NT, int V, bool EVEN, bool Z>
 __global__ __launch_bounds__(NT) void residual_grad_kernel(HopResidualTask t, HopIndex index) {
-    constexpr bool kKept = NT * V <= 1024;                  // 12 bytes of LDS a column: not for rows of over 8192
-    constexpr bool kAhead = NT * V <= 1024;                 // nor do the registers hold a second row there
+    typedef Vectors<NT, V> Vec;
+    constexpr bool kAhead = NT * V <= 1024;
     __shared__ float shared[4 * (NT / 64)];
-    __shared__ f32x4 kept[kKept ? 3 : 1][2 * V][kKept ? NT : 1];
+    __shared__ f32x4 kept[Vec::kKept ? 3 : 1][2 * V][Vec::kKept ? NT : 1];
     RowSums<NT> sums{shared, 0};
+    const Vec vec{kept};
     int g, r0, r1;
     if (!find_piece(t.rows, t.shift, blockIdx.x, &g, &r0, &r1)) return;
     const int at = t.indexed ? index.at[g] : g;
@@ -449,23 +452,18 @@ __global__ __launch_bounds__(NT) void residual_grad_kernel(HopResidualTask t, Ho
     auto global = [&](const float* p, int64_t stride, int i) {
         return p ? columns8(p + at * stride, t.cols, col[i] * 4, n[i]) : f32x8(1.f);
     };
-    if constexpr (kKept) {
+    auto read = [&](int w, int i) {
+        return w == 0 ? global(t.post, t.post_stride, i) : w == 1 ? global(t.pre, t.pre_stride, i) : global(t.gate, t.gate_stride, i);
+    };
+    if constexpr (Vec::kKept) {
 #pragma unroll
         for (int w = 0; w < 3; ++w)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const f32x8 v = w == 0 ? global(t.post, t.post_stride, i) : w == 1 ? global(t.pre, t.pre_stride, i) : global(t.gate, t.gate_stride, i);
-                kept[w][2 * i][threadIdx.x] = f32x4{v[0], v[1], v[2], v[3]};
-                kept[w][2 * i + 1][threadIdx.x] = f32x4{v[4], v[5], v[6], v[7]};
-            }
+            for (int i = 0; i < V; ++i) vec.put(w, i, read(w, i));
     }
     auto vector = [&](int w, int i) {
-        if constexpr (kKept) {
-            const f32x4 a = kept[w][2 * i][threadIdx.x], b = kept[w][2 * i + 1][threadIdx.x];
-            return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        } else {
-            return w == 0 ? global(t.post, t.post_stride, i) : w == 1 ? global(t.pre, t.pre_stride, i) : global(t.gate, t.gate_stride, i);
-        }
+        if constexpr (Vec::kKept) return vec.get(w, i);
+        else return read(w, i);
     };
     typedef Matrix<T, EVEN> M;
     const M mdy(t.dy, t.lddy, t.cols), mdh(t.dh, t.lddh, t.cols), my(t.dh ? t.y : nullptr, t.ldy, t.cols), mb(t.b, t.ldb, t.cols), mz(t.z, t.ldz, t.cols);
@@ -677,8 +675,10 @@ int hopl_residual(HopResidualTask t, int dtype, const HopIndex& index, void* str
     return (int)hipGetLastError();
 }
 
-// Gradient: a piece's sums have to be joined with the others', so few rows go in few pieces too (512 x 2048 in bf16: 512 pieces 26 us, 256 19;
-// 16384 x 4096: 1024 pieces 207 us, 512 182, 256 172; 16384 x 1024: 2048 pieces 82 us, 1024 63).
+// Gradient: a piece's sums have to be joined with the others', so few rows go in few pieces too.  At least 768 pieces of up to 1024 columns (bf16,
+// 16384 x 1024: 2048 pieces 84 us, 1024 65, 512 80; with fewer rows half as many would do: 4096 x 1024 39 and 35 us, 1000 x 256 with 1000 28,
+// with 250 17), 256 of up to 2048 (512 x 2048: 512 pieces 26 us, 256 19, 128 19; 16384: 1024 111, 512 100, 256 131), 192 beyond (777 x 5001 with
+// its 194 pieces 36 us, 388 45, 97 50; 16384 x 4096: 1024 pieces 206 us, 512 183, 256 170, 128 275).
 int hopl_grad_shift(int64_t rows, int64_t cols) {
     return shift_for(rows, cols <= 1024 ? 768 : cols <= 2048 ? 256 : 192);
 }
