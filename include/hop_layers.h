@@ -29,9 +29,9 @@
  *  - Calls enqueue kernels on `stream` and return (no allocation, no copy, no wait); they can be captured into a HIP graph.
  *    `scratch` is device memory, 16-byte aligned, of at least the bytes that the matching *_scratch_bytes call names (which may
  *    be 0); it is free again when the call's kernels have run.  Results are the same bits on every call with the same arguments.
- *  - Sizes: rows below 2^30 - 65536, products' columns up to 2^21 and results up to 2^40 elements, dropout's up to 2^29; anything else, like every null pointer, misaligned
- *    address, distance below the columns, unknown enum value and index below zero, is HOP_ERR_INVALID_ARG and nothing is launched; too
- *    little scratch is HOP_ERR_ARENA_TOO_SMALL.
+ *  - Sizes: rows below 2^30 - 65536, products' columns up to 2^21 and results up to 2^40 elements, dropout's columns up to 2^29; anything
+ *    else, like every null pointer, misaligned address, distance below the columns, unknown enum value and index below zero, is
+ *    HOP_ERR_INVALID_ARG and nothing is launched; too little scratch is HOP_ERR_ARENA_TOO_SMALL.
  *  - No rows (rows = 0): nothing is written except the gradients of parameters, which are zero.
  */
 #ifndef HOP_LAYERS_H
@@ -99,7 +99,7 @@ int hop_product_grad(const hop_product_grad_args* a, void* scratch, size_t scrat
  * Column c of a row takes 16 bits, word (c mod 8) / 2, low half first, and is kept if they are at least t = p * 65536 rounded
  * (half up); what is kept is multiplied by 65536 / (65536 - t), so the expectation is exact for the p that 16 bits can hold.
  * p = 0 keeps all, p = 1 nothing; what is dropped is 0 whatever it was.  `first_row` is the row number of the first row: a batch
- * cut in pieces has the mask of the whole. */
+ * cut in pieces has the mask of the whole.  A call has one mask, whatever its groups: workers with draws of their own are calls of their own. */
 typedef struct {
     uint64_t seed;
     int64_t first_row;
