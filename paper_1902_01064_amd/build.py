@@ -3,6 +3,7 @@
 `python -m paper_1902_01064_amd.build` compiles every time it is called; the
 binding only loads what is already built.
 """
+import concurrent.futures
 import os
 import subprocess
 import sys
@@ -30,16 +31,21 @@ def _run(cmd):
 def build_library():
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ, exist_ok=True)
-    objs = []
-    for src, extra in (("hop_kernels.hip", DEVICE),
-                       ("hop_product.hip", DEVICE),
-                       ("hop_residual.hip", DEVICE),
-                       ("hop_api.cpp", []),
-                       ("hop_layers.cpp", []),
-                       ("hop_sim.cpp", ["-ffp-contract=off"])):
-        o = os.path.join(OBJ, src + ".o")
-        _run([hipcc] + COMMON + extra + ["-c", os.path.join(CSRC, src), "-o", o])
-        objs.append(o)
+    sources = (("hop_kernels.hip", DEVICE),
+               ("hop_product.hip", DEVICE),
+               ("hop_attention.hip", DEVICE),
+               ("hop_attention_grad.hip", DEVICE),
+               ("hop_residual.hip", DEVICE),
+               ("hop_rotate.hip", DEVICE),
+               ("hop_api.cpp", []),
+               ("hop_layers.cpp", []),
+               ("hop_attention.cpp", []),
+               ("hop_sim.cpp", ["-ffp-contract=off"]))
+    objs = [os.path.join(OBJ, src + ".o") for src, _ in sources]
+    with concurrent.futures.ThreadPoolExecutor(min(6, os.cpu_count() or 1)) as pool:
+        for done in [pool.submit(_run, [hipcc] + COMMON + extra + ["-c", os.path.join(CSRC, src), "-o", o])
+                     for (src, extra), o in zip(sources, objs)]:
+            done.result()
     _run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950"] + objs + ["-o", LIB])
     return LIB
 

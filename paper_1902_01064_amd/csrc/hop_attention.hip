@@ -1,0 +1,276 @@
+// Softmax attention of packed sequences with grouped heads, for gfx950 (CDNA4).
+//
+//   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i k_j - lse_i),  lse_i = log sum_j exp(scale q_i k_j)     4 pairs cols operations
+//
+// A workgroup takes a run of a key head's pairs (query row, head of the group) and passes once over the keys that they see, tile by tile: scores
+// keys x pairs on the matrix unit, their running maximum and sum column by column, and the product of the values with the softmax's terms, which never
+// leave the registers.
+#include <algorithm>
+#include <type_traits>
+
+#include "hop_attention_device.h"
+
+using namespace hopa;
+
+namespace {
+
+template <typename T, int D>
+constexpr int kTileRows = D * (int)sizeof(T) <= 256 ? 64 : 32;
+
+// What a part of the keys leaves for each pair: an unnormalised sum, and the maximum (in powers of two) and the sum of its terms.
+__device__ __forceinline__ int64_t part_place(const HopAttentionTask& t, int part, int head, int64_t pair) {
+    return ((int64_t)part * t.k_heads + head) * ((int64_t)t.q_rows * t.group) + pair;
+}
+
+template <typename T, int D, bool FED, int NW, int NQ>
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 4 ? 1 : 2) void attention_kernel(HopAttentionTask t) {
+    typedef Tile<T, D> L;
+    constexpr int NT = NW * 64, kRows = kTileRows<T, D>, kBytes = kRows * L::kLine, kU = D / 32;
+    constexpr int kShift = (NW == 4 ? 7 : NW == 8 ? 8 : 5) + (NQ == 2);
+    static_assert(1 << kShift == NW * NQ * 32, "pairs of a workgroup");
+    // arrays of their own, so that the compiler knows that reads of one stage need not wait for loads into the other
+    __shared__ __attribute__((aligned(16))) char sk0[kBytes], sv0[kBytes], sk1[kBytes], sv1[kBytes];
+    const int head = blockIdx.x % t.k_heads, rest = blockIdx.x / t.k_heads, part = rest % t.parts;
+    int s, first;
+    if (!find_tile(t.q_begin, t.S, t.q_rows, t.group, kShift, true, rest / t.parts, &s, &first)) return;
+    const Sequence seq = sequence(t, s);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, hi = lane >> 5;
+    const int pairs = seq.nq * t.group, mine = first + wave * NQ * 32;       // the wavefront's first pair
+    const T* q = (const T*)t.q + seq.q0 * t.ldq + head * t.group * t.cols;
+    const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.cols;
+    const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.cols;
+
+    int limit[NQ];                             // keys that the lane's columns see
+    typename L::frag fq[NQ][L::kSteps];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int pair = mine + 32 * n + (lane & 31), row = divide(pair, t.group_inverse);
+        limit[n] = pair < pairs ? visible(seq, t.causal, row) : seq.nk;
+        load_columns<T, D, FED>(fq[n], q + row * t.ldq + (pair - row * t.group) * t.cols, t.cols, pair < pairs);
+    }
+    auto visible_of = [&](int pair) { return visible(seq, t.causal, divide(pair, t.group_inverse)); };
+    const int all_see = visible_of(mine), some_see = mine < pairs ? visible_of(min(mine + NQ * 32, pairs) - 1) : 0;
+    const int all_see_here = visible_of(first);                                       // of the workgroup's
+    const int chunk = (seq.nk + t.parts - 1) / t.parts, whole = (chunk + kRows - 1) / kRows * kRows;
+    const int64_t from = (int64_t)part * whole;
+    const int begin = from < seq.nk ? (int)from : seq.nk;
+    const int end = min(min(begin + whole, seq.nk), visible_of(min(first + (1 << kShift), pairs) - 1));
+
+    const Rows gk = {t.ldk, 1, 0, t.cols}, gv = {t.ldv, 1, 0, t.cols};
+    Feed<T, D, kRows, NT, FED, false> feed_k, feed_v;
+    auto issue = [&](char* sk, char* sv, int key) __attribute__((always_inline)) {
+        feed_k.issue(sk, k, gk, key, seq.nk - key);
+        feed_v.issue(sv, v, gv, key, seq.nk - key);
+    };
+    auto put = [&](char* sk, char* sv) __attribute__((always_inline)) {
+        feed_k.put(sk);
+        feed_v.put(sv);
+    };
+
+    f32x16 o[NQ][kU];
+    float top[NQ], sum[NQ];                    // of scores in powers of two; over the lane's own half of the column
+    auto turn = [&](const char* sk, const char* sv, int key) __attribute__((always_inline)) {
+        if (key >= some_see) return;
+#pragma unroll
+        for (int u = 0; u < kRows / 32; ++u) {
+            f32x16 p[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) p[n] = (f32x16)(0.f);
+#pragma unroll
+            for (int i = 0; i < L::kSteps; ++i) {
+                const typename L::frag a = L::along(sk, 32 * u, i);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) p[n] = multiply(a, fq[n][i], p[n]);
+            }
+            if (key + 32 * u + 32 > all_see) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (key + 32 * u + 8 * (r >> 2) + 4 * hi + (r & 3) >= limit[n]) p[n][r] = -kInf;
+            }
+            // The maximum is moved only when a score exceeds it by a factor of 2^8: terms of up to that are as exact, and most tiles leave the sums alone.
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                float most = p[n][0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) most = fmaxf(most, p[n][r]);
+                most = both_max(most) * t.scale_log2;
+                if (__any(most > top[n] + 8.f)) {
+                    const float now = fmaxf(top[n], most), by = now == -kInf ? 1.f : __builtin_amdgcn_exp2f(top[n] - now);
+                    top[n] = now;
+                    sum[n] *= by;
+#pragma unroll
+                    for (int c = 0; c < kU; ++c)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[n][c][e] *= by;
+                }
+                const float base = top[n] == -kInf ? 0.f : top[n];
+                float more = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    p[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][r], t.scale_log2, -base));
+                    more += p[n][r];
+                }
+                sum[n] += more;
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const Weights<T> w(p[n]);
+#pragma unroll
+                for (int c = 0; c < kU; ++c) o[n][c] = w.template product<D>(sv, 32 * u, c, o[n][c]);
+            }
+        }
+    };
+    auto careful_turn = [&](const char* sk, char* sv, int key) __attribute__((always_inline)) {
+        if (key + kRows > all_see_here) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+                add_not_finite<T, D>(sv, min(kRows, seq.nk - key), o[n], [&](int j) { return key + j < limit[n]; });
+            __syncthreads();
+            drop_not_finite<T, kBytes, NT>(sv);
+            __syncthreads();
+        }
+        turn(sk, sv, key);
+    };
+    auto pass = [&](auto careful) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            top[n] = -kInf;
+            sum[n] = 0.f;
+#pragma unroll
+            for (int c = 0; c < kU; ++c) o[n][c] = (f32x16)(0.f);
+        }
+        auto take = [&](const char* sk, char* sv, int key) __attribute__((always_inline)) {
+            if constexpr (decltype(careful)::value) careful_turn(sk, sv, key);
+            else turn(sk, sv, key);
+        };
+        if (begin < end) {
+            issue(sk0, sv0, begin);
+            put(sk0, sv0);
+        }
+        for (int key = begin; key < end; key += 2 * kRows) {
+            arrive();
+            const bool second = key + kRows < end, third = key + 2 * kRows < end;
+            if (second) issue(sk1, sv1, key + kRows);
+            take(sk0, sv0, key);
+            if (!second) break;
+            put(sk1, sv1);
+            arrive();
+            if (third) issue(sk0, sv0, key + 2 * kRows);
+            take(sk1, sv1, key + kRows);
+            if (third) put(sk0, sv0);
+        }
+    };
+    pass(std::false_type());
+    if (t.causal) {
+        bool fine = true;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) fine = fine && all_finite(o[n]);
+        if (__syncthreads_or(!fine)) pass(std::true_type());
+    }
+
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int pair = mine + 32 * n + (lane & 31), row = divide(pair, t.group_inverse);
+        const float total = both_sum(sum[n]), base = top[n] == -kInf ? 0.f : top[n];
+        if (pair >= pairs) continue;
+        const int column = (head * t.group + pair - row * t.group) * t.cols;
+        if (t.parts > 1) {
+            const int64_t at = part_place(t, part, head, (int64_t)seq.q0 * t.group + pair), all = part_place(t, t.parts, 0, 0);
+            store_columns<float, D>(t.partial + at * t.cols, t.cols, o[n], 1.f);
+            if (!hi) {
+                ((HOPL_GLOBAL float*)t.partial)[all * t.cols + 2 * at] = base;
+                ((HOPL_GLOBAL float*)t.partial)[all * t.cols + 2 * at + 1] = total;
+            }
+            continue;
+        }
+        store_columns<T, D>((T*)t.o + (seq.q0 + row) * t.ldo + column, t.cols, o[n], total == 0.f ? 0.f : 1.f / total);
+        if (t.lse && !hi)
+            ((HOPL_GLOBAL float*)t.lse)[(int64_t)(head * t.group + pair - row * t.group) * t.q_rows + seq.q0 + row] =
+                total == 0.f ? -kInf : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    }
+}
+
+// Joins the parts in their order: a wavefront per pair.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t) {
+    const int lane = threadIdx.x & 63;
+    const int64_t number = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), per_head = (int64_t)t.q_rows * t.group, all = part_place(t, t.parts, 0, 0);
+    const int head = (int)(number / per_head);
+    const int64_t pair = number - head * per_head;
+    const int row = (int)(pair / t.group), its = (int)(pair - (int64_t)row * t.group);
+    if (head >= t.k_heads) return;
+    int b = 0, e = t.q_rows;
+    if (t.q_begin) {
+        b = ((const HOPL_GLOBAL int32_t*)t.q_begin)[0];
+        e = ((const HOPL_GLOBAL int32_t*)t.q_begin)[t.S];
+    }
+    if (row < b || row >= e) return;
+    const HOPL_GLOBAL float* sums = (const HOPL_GLOBAL float*)t.partial;
+    const HOPL_GLOBAL float* tops = sums + all * t.cols;
+    float top = -kInf;
+    for (int p = 0; p < t.parts; ++p) {
+        const int64_t at = part_place(t, p, head, pair);
+        if (tops[2 * at + 1] != 0.f) top = fmaxf(top, tops[2 * at]);
+    }
+    float total = 0.f, v[2] = {0.f, 0.f};
+    for (int p = 0; p < t.parts; ++p) {
+        const int64_t at = part_place(t, p, head, pair);
+        if (tops[2 * at + 1] == 0.f) continue;
+        const float by = __builtin_amdgcn_exp2f(tops[2 * at] - top);
+        total += by * tops[2 * at + 1];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (lane + 64 * i < t.cols) v[i] += by * sums[at * t.cols + lane + 64 * i];
+    }
+    const float by = total == 0.f ? 0.f : 1.f / total;
+    const int h = head * t.group + its;
+    HOPL_GLOBAL T* o = (HOPL_GLOBAL T*)t.o + row * t.ldo + (int64_t)h * t.cols;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (lane + 64 * i < t.cols) o[lane + 64 * i] = (T)(v[i] * by);
+    if (t.lse && lane == 0) ((HOPL_GLOBAL float*)t.lse)[(int64_t)h * t.q_rows + row] = total == 0.f ? -kInf : (top + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+// Few pairs to a sequence: a wavefront takes them all.
+bool few(const HopAttentionTask& t) { return (int64_t)t.q_rows * t.group <= (int64_t)32 * t.S; }
+
+template <typename T, int D, bool FED>
+int launch(const HopAttentionTask& t, hipStream_t stream) {
+    const int64_t pairs = (int64_t)t.q_rows * t.group;
+    if (few(t)) {
+        const int64_t grid = ((pairs + 31) / 32 + t.S) * t.k_heads * t.parts;
+        attention_kernel<T, D, FED, 1, 1><<<dim3((unsigned)grid), dim3(64), 0, stream>>>(t);
+    } else {
+        const int64_t grid = ((pairs + 127) / 128 + t.S) * t.k_heads * t.parts;
+        attention_kernel<T, D, FED, 4, 1><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(t);
+    }
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && t.parts > 1) {
+        attention_join_kernel<T><<<dim3((unsigned)((pairs * t.k_heads + 3) / 4)), dim3(256), 0, stream>>>(t);
+        e = hipGetLastError();
+    }
+    return (int)e;
+}
+
+template <typename T>
+int launch(const HopAttentionTask& t, hipStream_t stream) {
+    auto fits = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && (ld * sizeof(T)) % 16 == 0; };
+    const bool fed = fits(t.q, t.ldq) && fits(t.k, t.ldk) && fits(t.v, t.ldv) && (t.cols * sizeof(T)) % 16 == 0;
+    if (t.cols <= 64) return fed ? launch<T, 64, true>(t, stream) : launch<T, 64, false>(t, stream);
+    return fed ? launch<T, 128, true>(t, stream) : launch<T, 128, false>(t, stream);
+}
+
+}  // namespace
+
+int hopa_forward_parts(const HopAttentionTask& t, int dtype) {
+    (void)dtype;
+    const int64_t step = few(t) ? 32 : 128, tiles = (((int64_t)t.q_rows * t.group + step - 1) / step + t.S) * t.k_heads, keys = t.k_rows / t.S;
+    const int64_t wanted = few(t) ? 1024 : 512;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((wanted + tiles - 1) / tiles, keys / 256), 64));
+}
+
+int hopa_forward(const HopAttentionTask& t, int dtype, void* stream) {
+    return dtype == HOP_BF16 ? launch<bf16>(t, (hipStream_t)stream) : launch<float>(t, (hipStream_t)stream);
+}

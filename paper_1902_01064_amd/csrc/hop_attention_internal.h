@@ -1,0 +1,59 @@
+// Internal declarations shared by the host side (hop_attention.cpp) and the kernels (hop_attention.hip, hop_attention_grad.hip,
+// hop_rotate.hip) of include/hop_attention.h.  Nothing here is part of the public ABI.
+#pragma once
+
+#include <cstdint>
+
+#include "hop_attention.h"
+#include "hop_layers_internal.h"
+
+// A head of queries and a row are a *pair*; the pairs of a key head's group are numbered row by row, head by head within a row, and the
+// kernels work on runs of pairs: every key and value that is read serves all heads of the group.
+struct HopAttentionTask {
+    const int32_t *q_begin, *k_begin;      // null: one sequence of all rows
+    int32_t S, q_rows, k_rows;
+    int32_t k_heads, group, cols;          // group: query heads of a key head
+    uint32_t group_inverse;                // ceil(2^32 / group), 0 for 1
+    int32_t causal, parts;
+    float scale, scale_log2;               // scale_log2 = scale log2(e)
+    const void *q, *k, *v;
+    int64_t ldq, ldk, ldv;
+    void* o;                               // forward (gradient: read)
+    int64_t ldo;
+    float* lse;
+    float* partial;                        // sums of parts of the contraction, see the kernels
+    const void* grad;                      // gradient
+    int64_t ldgrad;
+    void *dq, *dk, *dv;
+    int64_t lddq, lddk, lddv;
+    float* terms;                          // of every pair, [2][k_heads][q_rows group]: lse log2(e) and sum do o
+};
+
+struct HopRotateTask {
+    HopRows rows;
+    HopRows sequences;
+    const int32_t* positions;
+    int32_t q_heads, heads, cols, rotary, adjacent, norm, indexed, dindexed;
+    float eps, inv_cols;
+    const float *q_weight, *k_weight;
+    int64_t q_stride, k_stride;
+    const void *x, *dy;
+    void *y, *dx;
+    int64_t ldx, ldy, lddy, lddx;
+    float *dq_weight, *dk_weight;
+    int64_t dq_stride, dk_stride;
+    float* partial;                        // sums of the weights' gradients over the rows of a chunk: [chunk][2][cols]
+    int32_t shift;                         // rows of a chunk: 1 << shift
+    double turns[HOP_MAX_HEAD_COLS / 2];   // a pair's turns per position: base^(-2 i / rotary) / (2 pi)
+};
+
+int hopa_forward_parts(const HopAttentionTask& t, int dtype);
+int hopa_dq_parts(const HopAttentionTask& t, int dtype);
+int hopa_dkv_parts(const HopAttentionTask& t, int dtype);
+int hopa_forward(const HopAttentionTask& t, int dtype, void* stream);
+int hopa_grad(const HopAttentionTask& t, int dtype, int dq_parts, int dkv_parts, void* stream);
+
+int hopa_rotate(const HopRotateTask& t, int dtype, const HopIndex& index, void* stream);
+int hopa_rotate_grad(const HopRotateTask& t, int dtype, const HopIndex& index, const HopIndex& dindex, void* stream);
+int hopa_rotate_shift(int64_t rows, int32_t heads);
+int64_t hopa_rotate_chunks(int64_t rows, int G, int32_t heads);
