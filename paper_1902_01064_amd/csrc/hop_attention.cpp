@@ -98,21 +98,7 @@ bool attention_grads_ok(const hop_attention_args* a, const hop_attention_grads* 
         return false;
     return a->k_rows == 0 || (heads_ok(g->dk, g->lddk, narrow, e) && heads_ok(g->dv, g->lddv, narrow, e));
 }
-struct GradPlan {
-    int dq_parts, dkv_parts;
-    size_t terms, bytes;           // bytes of the terms, rounded up to 256; all together
-};
-GradPlan grad_plan(const hop_attention_args* a) {
-    const HopAttentionTask t = attention_task(a);
-    GradPlan p;
-    p.dq_parts = hopa_dq_parts(t, a->dtype);
-    p.dkv_parts = hopa_dkv_parts(t, a->dtype);
-    p.terms = ((size_t)2 * a->q_heads * a->q_rows * 4 + 255) / 256 * 256;
-    const size_t dq = p.dq_parts > 1 ? (size_t)p.dq_parts * a->q_rows * a->q_heads * a->cols * 4 : 0;
-    const size_t dkv = p.dkv_parts > 1 ? (size_t)p.dkv_parts * 2 * a->k_rows * a->k_heads * a->cols * 4 : 0;
-    p.bytes = p.terms + std::max(dq, dkv);
-    return p;
-}
+size_t term_bytes(const hop_attention_args* a) { return ((size_t)2 * a->q_heads * a->q_rows * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -181,24 +167,29 @@ int hop_attention(const hop_attention_args* a, void* o, int64_t ldo, float* lse,
 }
 
 size_t hop_attention_grad_scratch_bytes(const hop_attention_args* a, const hop_attention_grads* g) {
-    return attention_grads_ok(a, g) ? grad_plan(a).bytes : 0;
+    if (!attention_grads_ok(a, g) || (a->q_rows == 0 && a->k_rows == 0)) return 0;
+    const HopAttentionPlan p = hopa_grad_plan(attention_task(a), a->dtype);
+    return term_bytes(a) + p.q_bytes + p.k_bytes + p.partial_bytes;
 }
 
 int hop_attention_grad(const hop_attention_args* a, const hop_attention_grads* g, void* scratch, size_t scratch_bytes, void* stream) {
     if (!attention_grads_ok(a, g)) return HOP_ERR_INVALID_ARG;
     if (a->q_rows == 0 && a->k_rows == 0) return HOP_OK;
-    const GradPlan p = grad_plan(a);
-    if (scratch_bytes < p.bytes) return HOP_ERR_ARENA_TOO_SMALL;
-    if (p.bytes && (!scratch || ((uintptr_t)scratch & 15u))) return HOP_ERR_INVALID_ARG;
+    if (scratch_bytes < hop_attention_grad_scratch_bytes(a, g)) return HOP_ERR_ARENA_TOO_SMALL;
+    if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
     HopAttentionTask t = attention_task(a);
     t.grad = g->grad; t.ldgrad = g->ldgrad;
     t.o = const_cast<void*>(g->o); t.ldo = g->ldo;
     t.lse = const_cast<float*>(g->lse);
     t.dq = g->dq; t.dk = g->dk; t.dv = g->dv;
     t.lddq = g->lddq; t.lddk = g->lddk; t.lddv = g->lddv;
-    t.terms = (float*)scratch;
-    t.partial = (float*)((char*)scratch + p.terms);
-    const int rc = hopa_grad(t, a->dtype, p.dq_parts, p.dkv_parts, stream);
+    const HopAttentionPlan p = hopa_grad_plan(t, a->dtype);
+    char* at = (char*)scratch;
+    t.terms = (float*)at;
+    t.q_plan = at += term_bytes(a);
+    t.k_plan = at += p.q_bytes;
+    t.partial = (float*)(at + p.k_bytes);
+    const int rc = hopa_grad(t, a->dtype, p, stream);
     return rc ? hip_fail((hipError_t)rc, "attention gradient launch") : HOP_OK;
 }
 

@@ -17,39 +17,36 @@ namespace {
 template <typename T, int D>
 constexpr int kTileRows = D * (int)sizeof(T) <= 256 ? 64 : 32;
 
+
 // What a part of the keys leaves for each pair: an unnormalised sum, and the maximum (in powers of two) and the sum of its terms.
 __device__ __forceinline__ int64_t part_place(const HopAttentionTask& t, int part, int head, int64_t pair) {
     return ((int64_t)part * t.k_heads + head) * ((int64_t)t.q_rows * t.group) + pair;
 }
 
-template <typename T, int D, bool FED, int NW, int NQ>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 4 ? 1 : 2) void attention_kernel(HopAttentionTask t) {
+template <typename T, int D, bool FED, int NW>
+__global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 : 2) void attention_kernel(HopAttentionTask t) {
     typedef Tile<T, D> L;
     constexpr int NT = NW * 64, kRows = kTileRows<T, D>, kBytes = kRows * L::kLine, kU = D / 32;
-    constexpr int kShift = (NW == 4 ? 7 : NW == 8 ? 8 : 5) + (NQ == 2);
-    static_assert(1 << kShift == NW * NQ * 32, "pairs of a workgroup");
+    constexpr int kShift = NW == 4 ? 7 : 5, kAtOnce = sizeof(T) == 4 ? kRows / 32 : 1;
     // arrays of their own, so that the compiler knows that reads of one stage need not wait for loads into the other
     __shared__ __attribute__((aligned(16))) char sk0[kBytes], sv0[kBytes], sk1[kBytes], sv1[kBytes];
     const int head = blockIdx.x % t.k_heads, rest = blockIdx.x / t.k_heads, part = rest % t.parts;
     int s, first;
-    if (!find_tile(t.q_begin, t.S, t.q_rows, t.group, kShift, true, rest / t.parts, &s, &first)) return;
+    if (!find_tile<true>(t.q_begin, t.S, t.q_rows, t.group, kShift, rest / t.parts, &s, &first)) return;
     const Sequence seq = sequence(t, s);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, hi = lane >> 5;
-    const int pairs = seq.nq * t.group, mine = first + wave * NQ * 32;       // the wavefront's first pair
-    const T* q = (const T*)t.q + seq.q0 * t.ldq + head * t.group * t.cols;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hi = lane >> 5;
+    const int pairs = seq.nq * t.group, mine = first + wave * 32;            // the wavefront's first pair
+    const int pair = mine + (lane & 31);
+    const bool live = pair < pairs;
+    const int row = live ? divide(pair, t.group_inverse) : 0, its = live ? pair - row * t.group : 0;
+    const int limit = live ? visible(seq, t.causal, row) : seq.nk;             // keys that the lane's column sees
+    const T* q = (const T*)t.q + (seq.q0 + row) * t.ldq + (head * t.group + its) * t.cols;
     const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.cols;
     const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.cols;
-
-    int limit[NQ];                             // keys that the lane's columns see
-    typename L::frag fq[NQ][L::kSteps];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const int pair = mine + 32 * n + (lane & 31), row = divide(pair, t.group_inverse);
-        limit[n] = pair < pairs ? visible(seq, t.causal, row) : seq.nk;
-        load_columns<T, D, FED>(fq[n], q + row * t.ldq + (pair - row * t.group) * t.cols, t.cols, pair < pairs);
-    }
+    typename L::frag fq[L::kSteps];
+    load_columns<T, D, FED>(fq, q, t.cols, live);
     auto visible_of = [&](int pair) { return visible(seq, t.causal, divide(pair, t.group_inverse)); };
-    const int all_see = visible_of(mine), some_see = mine < pairs ? visible_of(min(mine + NQ * 32, pairs) - 1) : 0;
+    const int all_see = visible_of(mine), some_see = mine < pairs ? visible_of(min(mine + 32, pairs) - 1) : 0;
     const int all_see_here = visible_of(first);                                       // of the workgroup's
     const int chunk = (seq.nk + t.parts - 1) / t.parts, whole = (chunk + kRows - 1) / kRows * kRows;
     const int64_t from = (int64_t)part * whole;
@@ -58,6 +55,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 4 ? 1 : 2) void attention_ker
 
     const Rows gk = {t.ldk, 1, 0, t.cols}, gv = {t.ldv, 1, 0, t.cols};
     Feed<T, D, kRows, NT, FED, false> feed_k, feed_v;
+    feed_k.begin(gk, 0);
+    feed_v.begin(gv, 0);
     auto issue = [&](char* sk, char* sv, int key) __attribute__((always_inline)) {
         feed_k.issue(sk, k, gk, key, seq.nk - key);
         feed_v.issue(sv, v, gv, key, seq.nk - key);
@@ -67,129 +66,126 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 4 ? 1 : 2) void attention_ker
         feed_v.put(sv);
     };
 
-    f32x16 o[NQ][kU];
-    float top[NQ], sum[NQ];                    // of scores in powers of two; over the lane's own half of the column
+    f32x16 o[kU];
+    float top, sum;                            // of scores in powers of two; over the lane's own half of the column
+    auto clear = [&]() __attribute__((always_inline)) {
+        top = -kInf;
+        sum = 0.f;
+#pragma unroll
+        for (int c = 0; c < kU; ++c) o[c] = (f32x16)(0.f);
+    };
+    // N units of 32 keys at once: what one waits for, another fills.  In fp32 (32 sequences of 128 rows: 27.7 us, one by one 32.7); operands of bfloat16 need the
+    // registers for other things (a prompt of 8192 rows: 235 us, one by one 203).
+    auto units = [&](auto n, const char* sk, const char* sv, int key) __attribute__((always_inline)) {
+        constexpr int N = decltype(n)::value;
+        f32x16 p[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) p[u] = (f32x16)(0.f);
+#pragma unroll
+        for (int i = 0; i < L::kSteps; ++i)
+#pragma unroll
+            for (int u = 0; u < N; ++u) p[u] = multiply(L::along(sk, 32 * u, i), fq[i], p[u]);
+        if (key + 32 * N > all_see) {
+            asm volatile("");                  // a branch, which few tiles take, and not selections that all of them make
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (key + 32 * u + 8 * (r >> 2) + 4 * hi + (r & 3) >= limit) p[u][r] = -kInf;
+        }
+        // The maximum is moved only when a score exceeds it by a factor of 2^8: terms of up to that are as exact, and most tiles leave the sums alone.
+        float most = p[0][0];
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, p[u][r]);
+        if (__any(__builtin_fmaf(most, t.scale_log2, -8.f) > top)) {
+            const float now = fmaxf(top, both_max(most) * t.scale_log2), by = now == -kInf ? 1.f : __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            sum *= by;
+#pragma unroll
+            for (int c = 0; c < kU; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[c][e] *= by;
+        }
+        const float base = top == -kInf ? 0.f : top;
+        float more[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                p[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[u][r], t.scale_log2, -base));
+                more[r & 3] += p[u][r];
+            }
+        sum += (more[0] + more[1]) + (more[2] + more[3]);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const Weights<T> w(p[u]);
+            Sums<T, D, false> sums;
+            sums.begin(sv + 32 * u * L::kLine, sv);
+            sums.add(sv + 32 * u * L::kLine, sv, w, w, o, o);
+        }
+    };
     auto turn = [&](const char* sk, const char* sv, int key) __attribute__((always_inline)) {
-        if (key >= some_see) return;
 #pragma unroll
-        for (int u = 0; u < kRows / 32; ++u) {
-            f32x16 p[NQ];
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) p[n] = (f32x16)(0.f);
-#pragma unroll
-            for (int i = 0; i < L::kSteps; ++i) {
-                const typename L::frag a = L::along(sk, 32 * u, i);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) p[n] = multiply(a, fq[n][i], p[n]);
-            }
-            if (key + 32 * u + 32 > all_see) {
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (key + 32 * u + 8 * (r >> 2) + 4 * hi + (r & 3) >= limit[n]) p[n][r] = -kInf;
-            }
-            // The maximum is moved only when a score exceeds it by a factor of 2^8: terms of up to that are as exact, and most tiles leave the sums alone.
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                float most = p[n][0];
-#pragma unroll
-                for (int r = 1; r < 16; ++r) most = fmaxf(most, p[n][r]);
-                most = both_max(most) * t.scale_log2;
-                if (__any(most > top[n] + 8.f)) {
-                    const float now = fmaxf(top[n], most), by = now == -kInf ? 1.f : __builtin_amdgcn_exp2f(top[n] - now);
-                    top[n] = now;
-                    sum[n] *= by;
-#pragma unroll
-                    for (int c = 0; c < kU; ++c)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[n][c][e] *= by;
-                }
-                const float base = top[n] == -kInf ? 0.f : top[n];
-                float more = 0.f;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    p[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][r], t.scale_log2, -base));
-                    more += p[n][r];
-                }
-                sum[n] += more;
-            }
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                const Weights<T> w(p[n]);
-#pragma unroll
-                for (int c = 0; c < kU; ++c) o[n][c] = w.template product<D>(sv, 32 * u, c, o[n][c]);
-            }
+        for (int u = 0; u < kRows / 32; u += kAtOnce) {
+            if (key + 32 * u >= some_see) break;
+            if (kAtOnce > 1 && key + 32 * (u + 1) >= some_see) units(std::integral_constant<int, 1>(), sk + 32 * u * L::kLine, sv + 32 * u * L::kLine, key + 32 * u);
+            else units(std::integral_constant<int, kAtOnce>(), sk + 32 * u * L::kLine, sv + 32 * u * L::kLine, key + 32 * u);
         }
     };
-    auto careful_turn = [&](const char* sk, char* sv, int key) __attribute__((always_inline)) {
-        if (key + kRows > all_see_here) {
-#pragma unroll
-            for (int n = 0; n < NQ; ++n)
-                add_not_finite<T, D>(sv, min(kRows, seq.nk - key), o[n], [&](int j) { return key + j < limit[n]; });
-            __syncthreads();
-            drop_not_finite<T, kBytes, NT>(sv);
-            __syncthreads();
-        }
-        turn(sk, sv, key);
-    };
-    auto pass = [&](auto careful) __attribute__((always_inline)) {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            top[n] = -kInf;
-            sum[n] = 0.f;
-#pragma unroll
-            for (int c = 0; c < kU; ++c) o[n][c] = (f32x16)(0.f);
-        }
-        auto take = [&](const char* sk, char* sv, int key) __attribute__((always_inline)) {
-            if constexpr (decltype(careful)::value) careful_turn(sk, sv, key);
-            else turn(sk, sv, key);
-        };
-        if (begin < end) {
-            issue(sk0, sv0, begin);
-            put(sk0, sv0);
-        }
-        for (int key = begin; key < end; key += 2 * kRows) {
-            arrive();
-            const bool second = key + kRows < end, third = key + 2 * kRows < end;
-            if (second) issue(sk1, sv1, key + kRows);
-            take(sk0, sv0, key);
-            if (!second) break;
-            put(sk1, sv1);
-            arrive();
-            if (third) issue(sk0, sv0, key + 2 * kRows);
-            take(sk1, sv1, key + kRows);
-            if (third) put(sk0, sv0);
-        }
-    };
-    pass(std::false_type());
+    clear();
+    if (begin < end) {
+        issue(sk0, sv0, begin);
+        put(sk0, sv0);
+    }
+    for (int key = begin; key < end; key += 2 * kRows) {
+        arrive();
+        const bool second = key + kRows < end, third = key + 2 * kRows < end;
+        if (second) issue(sk1, sv1, key + kRows);
+        turn(sk0, sv0, key);
+        if (!second) break;
+        put(sk1, sv1);
+        arrive();
+        if (third) issue(sk0, sv0, key + 2 * kRows);
+        turn(sk1, sv1, key + kRows);
+        if (third) put(sk0, sv0);
+    }
     if (t.causal) {
-        bool fine = true;
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) fine = fine && all_finite(o[n]);
-        if (__syncthreads_or(!fine)) pass(std::true_type());
+        if (__syncthreads_or(live && !all_finite(o))) {
+            clear();
+            for (int key = begin; key < end; key += kRows) {
+                issue(sk0, sv0, key);
+                put(sk0, sv0);
+                arrive();
+                if (key + kRows > all_see_here) {
+                    add_not_finite<T, D>(sv0, min(kRows, seq.nk - key), o, [&](int j) { return key + j < limit; });
+                    __syncthreads();
+                    drop_not_finite<T, kBytes, NT>(sv0);
+                    __syncthreads();
+                }
+                turn(sk0, sv0, key);
+                __syncthreads();
+            }
+        }
     }
 
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const int pair = mine + 32 * n + (lane & 31), row = divide(pair, t.group_inverse);
-        const float total = both_sum(sum[n]), base = top[n] == -kInf ? 0.f : top[n];
-        if (pair >= pairs) continue;
-        const int column = (head * t.group + pair - row * t.group) * t.cols;
-        if (t.parts > 1) {
-            const int64_t at = part_place(t, part, head, (int64_t)seq.q0 * t.group + pair), all = part_place(t, t.parts, 0, 0);
-            store_columns<float, D>(t.partial + at * t.cols, t.cols, o[n], 1.f);
-            if (!hi) {
-                ((HOPL_GLOBAL float*)t.partial)[all * t.cols + 2 * at] = base;
-                ((HOPL_GLOBAL float*)t.partial)[all * t.cols + 2 * at + 1] = total;
-            }
-            continue;
+    const float total = both_sum(sum), base = top == -kInf ? 0.f : top;
+    if (!live) return;
+    if (t.parts > 1) {
+        const int64_t at = part_place(t, part, head, (int64_t)seq.q0 * t.group + pair), all = part_place(t, t.parts, 0, 0);
+        store_columns<float, D>(t.partial + at * t.cols, t.cols, o, 1.f);
+        if (!hi) {
+            ((HOPL_GLOBAL float*)t.partial)[all * t.cols + 2 * at] = base;
+            ((HOPL_GLOBAL float*)t.partial)[all * t.cols + 2 * at + 1] = total;
         }
-        store_columns<T, D>((T*)t.o + (seq.q0 + row) * t.ldo + column, t.cols, o[n], total == 0.f ? 0.f : 1.f / total);
-        if (t.lse && !hi)
-            ((HOPL_GLOBAL float*)t.lse)[(int64_t)(head * t.group + pair - row * t.group) * t.q_rows + seq.q0 + row] =
-                total == 0.f ? -kInf : (base + __builtin_amdgcn_logf(total)) * kLn2;
+        return;
     }
+    const int column = (head * t.group + its) * t.cols;
+    store_columns<T, D>((T*)t.o + (seq.q0 + row) * t.ldo + column, t.cols, o, total == 0.f ? 0.f : 1.f / total);
+    if (t.lse && !hi)
+        ((HOPL_GLOBAL float*)t.lse)[(int64_t)(head * t.group + its) * t.q_rows + seq.q0 + row] =
+            total == 0.f ? -kInf : (base + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 // Joins the parts in their order: a wavefront per pair.
@@ -241,10 +237,10 @@ int launch(const HopAttentionTask& t, hipStream_t stream) {
     const int64_t pairs = (int64_t)t.q_rows * t.group;
     if (few(t)) {
         const int64_t grid = ((pairs + 31) / 32 + t.S) * t.k_heads * t.parts;
-        attention_kernel<T, D, FED, 1, 1><<<dim3((unsigned)grid), dim3(64), 0, stream>>>(t);
+        attention_kernel<T, D, FED, 1><<<dim3((unsigned)grid), dim3(64), 0, stream>>>(t);
     } else {
         const int64_t grid = ((pairs + 127) / 128 + t.S) * t.k_heads * t.parts;
-        attention_kernel<T, D, FED, 4, 1><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(t);
+        attention_kernel<T, D, FED, 4><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(t);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && t.parts > 1) {

@@ -34,10 +34,11 @@ struct Tile {
         if (kLine == 128) return ((r >> 1 & 1) << 2) | (r >> 2 & 3);
         return ((r & 3) << 2) | (r >> 2 & 3);
     }
-    // The first operand of a product over columns: lane l holds row l % 32, chunk 2 step + l / 32.
+    // The first operand of a product over columns: lane l holds row l % 32, chunk 2 step + l / 32.  Places are a number of the lane's, with a constant's bits flipped,
+    // and a constant behind it, so that few registers hold the addresses of all reads.
     static __device__ __forceinline__ frag along(const char* s, int row0, int step) {
-        const int lane = threadIdx.x & 63, row = row0 + (lane & 31), c = step * 2 + (lane >> 5);
-        return *(const frag*)(s + row * kLine + ((c ^ swizzle(row)) << 4));
+        const int lane = threadIdx.x & 63, row = lane & 31, place = row * kLine + (((lane >> 5) ^ swizzle(row)) << 4);
+        return *(const frag*)(s + (place ^ (step * 32)) + row0 * kLine);
     }
 };
 
@@ -48,14 +49,15 @@ __device__ __forceinline__ f32x16 multiply(f32x4 a, f32x4 b, f32x16 c) {
     return c;
 }
 
-// An accumulator as the second operand of a product over its rows, and that product: c[column][.] += sum over 32 rows of a tile from row0 on.
+// An accumulator as the second operand of a product over its rows: two parts of 16 rows.  `across` reads the first operand, of a tile's rows from row0 on and 32 columns.
 // bf16: part u holds rows 16 u + 4 (lane / 32) + e and, from element 4 on, 8 more; the transposing read brings the tile's in the same order (16 lanes hold
-// four rows of 16 columns each, lane l of them gets column l).
+// four rows of 16 columns each, lane l of them gets column l).  fp32: an element to a product.
 template <typename T>
 struct Weights;
 template <>
 struct Weights<bf16> {
-    bf16x8 part[2];
+    typedef bf16x8 Part;
+    Part part[2];
     __device__ __forceinline__ explicit Weights(const f32x16& p) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -63,43 +65,114 @@ struct Weights<bf16> {
             for (int e = 0; e < 8; ++e) part[u][e] = (bf16)p[8 * u + e];     // to nearest, ties to even
     }
     template <int D>
-    __device__ __forceinline__ f32x16 product(const char* s, int row0, int unit, f32x16 c) const {
+    static __device__ __forceinline__ Part across(const char* s, int row0, int unit, int u) {
         typedef Tile<bf16, D> L;
-        const int lane = threadIdx.x & 63, col = 32 * unit + (lane & 16) + (lane & 3) * 4;
+        const int lane = threadIdx.x & 63, row = 4 * (lane >> 5) + (lane >> 2 & 3);
+        const int place = row * L::kLine + (((lane >> 4 & 1) * 2 + (lane >> 1 & 1) ^ L::swizzle(row)) << 4) + (lane & 1) * 8;
+        union { s16x4 half[2]; bf16x8 all; } a;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            union { s16x4 half[2]; bf16x8 all; } a;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = row0 + 16 * u + 8 * h + 4 * (lane >> 5) + (lane >> 2 & 3);
-                const char* at = s + row * L::kLine + (((col >> 3) ^ L::swizzle(row)) << 4) + (col & 4) * 2;
-                a.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
-            }
-            c = multiply(a.all, part[u], c);
+        for (int h = 0; h < 2; ++h) {
+            const char* at = s + (place ^ (unit * 64 + h * 32)) + (row0 + 16 * u + 8 * h) * L::kLine;
+            a.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
         }
-        return c;
+        return a.all;
     }
+    static __device__ __forceinline__ f32x16 add(const Part& a, const Part& b, f32x16 c) { return multiply(a, b, c); }
 };
 template <>
 struct Weights<float> {
-    f32x16 p;
-    __device__ __forceinline__ explicit Weights(const f32x16& p_) : p(p_) {}
-    template <int D>
-    __device__ __forceinline__ f32x16 product(const char* s, int row0, int unit, f32x16 c) const {
-        typedef Tile<float, D> L;
-        const int lane = threadIdx.x & 63, col = 32 * unit + (lane & 31);
+    typedef f32x8 Part;
+    Part part[2];
+    __device__ __forceinline__ explicit Weights(const f32x16& p) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = row0 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-            const float a = *(const float*)(s + row * L::kLine + (((col >> 2) ^ L::swizzle(row)) << 4) + (col & 3) * 4);
-            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[r], c, 0, 0, 0);
-        }
+        for (int e = 0; e < 16; ++e) part[e >> 3][e & 7] = p[e];
+    }
+    template <int D>
+    static __device__ __forceinline__ Part across(const char* s, int row0, int unit, int u) {
+        typedef Tile<float, D> L;
+        const int lane = threadIdx.x & 63, hi = lane >> 5, place = 4 * hi * L::kLine + (((lane & 31) >> 2 ^ hi << 3) << 4) + (lane & 3) * 4;
+        Part a;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) a[r] = *(const float*)(s + (place ^ (unit * 128 + r * 16)) + (row0 + 16 * u + 8 * (r >> 2) + (r & 3)) * L::kLine);
+        return a;
+    }
+    static __device__ __forceinline__ f32x16 add(const Part& a, const Part& b, f32x16 c) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
         return c;
     }
 };
 
+// ---- products in turn with other things -----------------------------------------------------
+// Left to itself the compiler reads an operand right in front of the product that wants it, so that every product waits for LDS, and puts all arithmetic behind
+// all products.  Here the order is written down: operands are read kAhead products early, and between two of them the matrix unit has a share of other work beside it.
+//
+// Scores of 32 rows of one or two tiles with the columns c0 (c1): beside(e) is called for e = 0 .. 15 in between.
+template <typename T, int D, bool TWO, typename BESIDE>
+__device__ __forceinline__ void scores_beside(const char* s0, const char* s1, const typename Tile<T, D>::frag* c0, const typename Tile<T, D>::frag* c1, f32x16& r0, f32x16& r1,
+                                              BESIDE beside) {
+    typedef Tile<T, D> L;
+    constexpr int kN = L::kSteps, kAhead = sizeof(T) == 4 ? 2 : 4;
+    typename L::frag a0[kAhead], a1[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        a0[i] = L::along(s0, 0, i);
+        if constexpr (TWO) a1[i] = L::along(s1, 0, i);
+    }
+    r0 = (f32x16)(0.f);
+    if constexpr (TWO) r1 = (f32x16)(0.f);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        r0 = multiply(a0[i % kAhead], c0[i], r0);
+        if constexpr (TWO) r1 = multiply(a1[i % kAhead], c1[i], r1);
+        if (i + kAhead < kN) {
+            a0[i % kAhead] = L::along(s0, 0, i + kAhead);
+            if constexpr (TWO) a1[i % kAhead] = L::along(s1, 0, i + kAhead);
+        }
+#pragma unroll
+        for (int e = i * 16 / kN; e < (i + 1) * 16 / kN; ++e) beside(e);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// c0[column][.] += sum over 32 rows of tile s0 times w0, and the same of c1, s1, w1.  `begin` reads the first operands.
+template <typename T, int D, bool TWO>
+struct Sums {
+    typedef Weights<T> W;
+    static constexpr int kU = D / 32, kN = kU * (TWO ? 4 : 2), kAhead = sizeof(T) == 4 ? 2 : kN < 6 ? kN : 6;
+    typename W::Part a[kAhead];
+    // Products in an order in which neighbours have different sums: both tiles', or two columns'.
+    static __device__ __forceinline__ void item(int k, int* which, int* unit, int* u) {
+        *which = TWO ? k & 1 : 0;
+        *u = k >> 1 & 1;
+        *unit = TWO ? k >> 2 : (k >> 2) * 2 + (k & 1);
+    }
+    static __device__ __forceinline__ typename W::Part read(const char* s0, const char* s1, int k) {
+        int which, unit, u;
+        item(k, &which, &unit, &u);
+        return W::template across<D>(which ? s1 : s0, 0, unit, u);
+    }
+    __device__ __forceinline__ void begin(const char* s0, const char* s1) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) a[k] = read(s0, s1, k);
+    }
+    __device__ __forceinline__ void add(const char* s0, const char* s1, const W& w0, const W& w1, f32x16* c0, f32x16* c1) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+            int which, unit, u;
+            item(k, &which, &unit, &u);
+            f32x16& c = which ? c1[unit] : c0[unit];
+            c = W::add(a[k % kAhead], (which ? w1 : w0).part[u], c);
+            if (k + kAhead < kN) a[k % kAhead] = read(s0, s1, k + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
 // ---- from memory to tiles ---------------------------------------------------------------
-__device__ __forceinline__ int divide(int x, uint32_t inverse) { return inverse ? (int)__umulhi((uint32_t)x, inverse) : x; }
+__device__ __forceinline__ int divide(int x, uint32_t inverse) { return (int)(__umulhi((uint32_t)x, inverse) + ((uint32_t)x & (inverse ? 0u : ~0u))); }
 
 // Where the rows of a tile lie: rows of keys, `ld` apart; or pairs, whose group's heads lie beside each other in a row.
 struct Rows {
@@ -111,15 +184,34 @@ struct Rows {
 
 // FED: addresses and distances are multiples of 16 bytes, and so are the heads: the memory unit fills the tile itself, through a buffer descriptor whose end
 // is that of the rows that there are (what lies outside comes back as zero).  Else through registers, by 128-bit loads at an element's address.
+// A lane's places in a tile are worked out once, and for pairs again where a tile begins with another head than the one before.
 template <typename T, int D, int ROWS, int NT, bool FED, bool PAIRS>
 struct Feed {
     typedef Tile<T, D> L;
     static constexpr int kLoads = ROWS * L::kPlaces / NT;
+    uint32_t place[kLoads];                     // FED: bytes behind the tile's first row; else elements
     typename L::frag held[FED ? 1 : kLoads];
+    int rest;
 
+    static __device__ __forceinline__ int line(int i) { return (i * NT + (int)threadIdx.x) / L::kPlaces; }
+    static __device__ __forceinline__ int chunk(int i) {
+        const int j = i * NT + threadIdx.x;
+        return FED ? (j % L::kPlaces) ^ L::swizzle(j / L::kPlaces) : j % L::kPlaces;
+    }
+    // rest_: how many heads of the first row belong to pairs in front of the tile
+    __device__ __forceinline__ void begin(const Rows& g, int rest_) {
+        rest = rest_;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int l = line(i), c = chunk(i) * L::kChunk, row = PAIRS ? divide(rest + l, g.inverse) : l;
+            const uint32_t at = (uint32_t)row * (uint32_t)g.ld + (PAIRS ? (rest + l - row * g.group) * g.cols : 0) + c;
+            place[i] = FED ? (c >= g.cols ? kOutside : at * (uint32_t)sizeof(T)) : at;
+        }
+    }
     // rows first, first + 1, ... (numbers of rows, or of pairs), `count` (at least 1) of them exist; base: row 0's first column of the head or the group
     __device__ __forceinline__ void issue(char* stage, const T* base, const Rows& g, int first, int count) {
-        const int row0 = PAIRS ? divide(first, g.inverse) : first, rest = PAIRS ? first - row0 * g.group : 0;
+        const int row0 = PAIRS ? divide(first, g.inverse) : first;
+        if (PAIRS && first - row0 * g.group != rest) begin(g, first - row0 * g.group);
         const T* from = base + row0 * g.ld;
         if (count > ROWS) count = ROWS;
         if constexpr (FED) {
@@ -127,33 +219,22 @@ struct Feed {
             const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(end * sizeof(T)), 0x00020000);
             const int wave = threadIdx.x >> 6;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int j = i * NT + threadIdx.x, l = j / L::kPlaces, c = (j % L::kPlaces) ^ L::swizzle(l);
-                const int row = PAIRS ? divide(rest + l, g.inverse) : l;
-                uint32_t o = (uint32_t)(row * (uint32_t)g.ld + (PAIRS ? (rest + l - row * g.group) * g.cols : 0)) * sizeof(T) + c * 16;
-                if (c * L::kChunk >= g.cols || l >= count) o = kOutside;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(stage + (i * NT + wave * 64) * 16), 16, o, 0, 0, 0);
-            }
+            for (int i = 0; i < kLoads; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(stage + (i * NT + wave * 64) * 16), 16, place[i], 0, 0, 0);
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int j = i * NT + threadIdx.x, l = j / L::kPlaces, c = j % L::kPlaces * L::kChunk, n = g.cols - c;
-                const int row = PAIRS ? divide(rest + l, g.inverse) : l;
+                const int n = line(i) < count ? g.cols - chunk(i) * L::kChunk : 0;
                 held[i] = (T)0.f;
-                if (l >= count || n <= 0) continue;
-                const T* p = from + row * g.ld + (PAIRS ? (rest + l - row * g.group) * g.cols : 0) + c;
-                if (n >= L::kChunk) held[i] = *(const HOPL_GLOBAL typename L::frag_any*)p;
-                else held[i] = load_short<typename L::frag>(p, n);
+                if (n >= L::kChunk) held[i] = *(const HOPL_GLOBAL typename L::frag_any*)(from + place[i]);
+                else if (n > 0) held[i] = load_short<typename L::frag>(from + place[i], n);
             }
         }
     }
     __device__ __forceinline__ void put(char* stage) {
         if constexpr (!FED) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int j = i * NT + threadIdx.x, l = j / L::kPlaces, c = (j % L::kPlaces) ^ L::swizzle(l);
-                *(typename L::frag*)(stage + l * L::kLine + c * 16) = held[i];
-            }
+            for (int i = 0; i < kLoads; ++i) *(typename L::frag*)(stage + line(i) * L::kLine + ((chunk(i) ^ L::swizzle(line(i))) << 4)) = held[i];
         }
     }
 };
@@ -279,15 +360,16 @@ __device__ __forceinline__ void rows_of(const int32_t* begin, int s, int rows, i
     *n = clamp_int(table[s + 1], *b, rows) - *b;
 }
 
-// Tile number `tile` of the sequences' rows, 1 << shift (times `by` a row) to a tile: its sequence and first row (or pair).  `back`: from the last
-// sequence's last tile on.  False: there are fewer.  Every wavefront works it out for itself, 64 sequences at a time.
-__device__ __forceinline__ bool find_tile(const int32_t* begin, int S, int rows, int by, int shift, bool back, int tile, int* s, int* first) {
+// Tile number `tile` of the sequences' rows, 1 << shift (times `by` a row) to a tile: its sequence and first row (or pair).  False: there are fewer.
+// Every wavefront works it out for itself, 64 sequences at a time.  DEEP: within 64 sequences in the order of the place in the sequence, the farthest first; where queries
+// see what is in front of them those have most to do, and what begins last is to be short.
+template <bool DEEP>
+__device__ __forceinline__ bool find_tile(const int32_t* begin, int S, int rows, int by, int shift, int tile, int* s, int* first) {
     const int lane = threadIdx.x & 63, step = 1 << shift;
     int seen = 0;
     for (int base = 0; base < S; base += 64) {
-        const int mine = back ? S - 1 - (base + lane) : base + lane;
         int b = 0, n = 0;
-        if (base + lane < S) rows_of(begin, mine, rows, &b, &n);
+        if (base + lane < S) rows_of(begin, base + lane, rows, &b, &n);
         const int tiles = (int)(((int64_t)n * by + step - 1) >> shift);
         int scan = tiles;
 #pragma unroll
@@ -295,16 +377,54 @@ __device__ __forceinline__ bool find_tile(const int32_t* begin, int S, int rows,
             const int before = __shfl_up(scan, o);
             if (lane >= o) scan += before;
         }
-        const uint64_t behind = __ballot(seen + scan > tile);
-        if (behind) {
+        const int all = __builtin_amdgcn_readlane(scan, 63);
+        if (tile - seen >= all) {
+            seen += all;
+            continue;
+        }
+        if (!DEEP || S == 1) {
+            const uint64_t behind = __ballot(seen + scan > tile);
+            if (!behind) return false;                        // only where a broken table made the sums overflow
             const int l = __builtin_ctzll(behind), its = __builtin_amdgcn_readlane(tiles, l);
             const int at = tile - (seen + __builtin_amdgcn_readlane(scan, l) - its);
-            if (at < 0 || at >= its) return false;            // only where a broken table made the sums overflow
-            *s = back ? S - 1 - (base + l) : base + l;
-            *first = (back ? its - 1 - at : at) << shift;
+            if (at < 0 || at >= its) return false;
+            *s = base + l;
+            *first = (DEEP ? its - 1 - at : at) << shift;
             return true;
         }
-        seen += __builtin_amdgcn_readlane(scan, 63);
+        // the deepest place from which on there are more tiles than that
+        auto from = [&](int depth) {
+            int k = tiles > depth ? tiles - depth : 0;
+#pragma unroll
+            for (int o = 32; o; o >>= 1) k += __shfl_xor(k, o);
+            return __builtin_amdgcn_readfirstlane(k);
+        };
+        const int at = tile - seen;
+        int low = 0, high = 1;                                // from(low) > at >= from(high)
+        int behind_high;
+        while ((behind_high = from(high)) > at) {
+            low = high;
+            high = high < 1 << 29 ? 2 * high : 0x7FFFFFFF;
+        }
+        while (high - low > 1) {
+            const int middle = low + (high - low) / 2, k = from(middle);
+            if (k > at) low = middle;
+            else {
+                high = middle;
+                behind_high = k;
+            }
+        }
+        uint64_t there = __ballot(tiles > low);
+        int l = -1;
+        for (int skip = at - behind_high; there; there &= there - 1)
+            if (skip-- == 0) {
+                l = __builtin_ctzll(there);
+                break;
+            }
+        if (l < 0) return false;
+        *s = base + l;
+        *first = low << shift;
+        return true;
     }
     return false;
 }
@@ -321,5 +441,106 @@ __device__ __forceinline__ Sequence sequence(const HopAttentionTask& t, int s) {
 }
 // How many keys of its sequence a row of queries sees.
 __device__ __forceinline__ int visible(const Sequence& q, int causal, int row) { return causal ? clamp_int(row + 1 + q.nk - q.nq, 0, q.nk) : q.nk; }
+
+
+// ---- a pipeline over stages -----------------------------------------------------------------
+// n stages of U units through three buffers, one barrier a stage: while a stage is worked on, the next one has arrived or is on its way, and every
+// step starts the products of the unit that follows (`step(i, buffer, unit, buffer of the next unit, next unit)`) beside the arithmetic of its own, which
+// otherwise would wait for one another within a wavefront.  The unit behind the last one is whatever lies in LDS; nobody uses its scores.
+// The buffers are three restricted pointers, so that the compiler knows that reads of one need not wait for loads into another.
+template <int U, typename ISSUE, typename FIRST, typename STEP>
+__device__ __forceinline__ void pipeline_begin(char* __restrict now, char* __restrict next, int n, ISSUE issue, FIRST first, STEP step) {
+    if (n > 1) issue(next, 1);
+    first(now);
+#pragma unroll
+    for (int u = 0; u + 1 < U; ++u) step(0, now, u, now, u + 1);
+}
+// The last unit of a stage and all but the last of the next one.
+template <int U, typename ISSUE, typename PUT, typename STEP>
+__device__ __forceinline__ void pipeline_turn(char* __restrict now, char* __restrict next, char* __restrict after, int i, int n, ISSUE issue, PUT put, STEP step) {
+    if (i + 1 < n) put(next);
+    arrive();                                   // the next stage is there, and nobody reads from the one before this any more
+    if (i + 2 < n) issue(after, i + 2);
+    step(i, now, U - 1, next, 0);
+    if (i + 1 < n)
+#pragma unroll
+        for (int u = 0; u + 1 < U; ++u) step(i + 1, next, u, next, u + 1);
+}
+template <int U, typename ISSUE, typename PUT, typename FIRST, typename STEP>
+__device__ __forceinline__ void pipeline(int n, char* pool, int bytes, ISSUE issue, PUT put, FIRST first, STEP step) {
+    char *now = pool, *next = pool + bytes, *after = pool + 2 * bytes;
+    __syncthreads();                            // with whoever still reads from the buffers
+    issue(now, 0);
+    put(now);
+    arrive();
+    pipeline_begin<U>(now, next, n, issue, first, step);
+    for (int i = 0; i < n; ++i) {
+        pipeline_turn<U>(now, next, after, i, n, issue, put, step);
+        char* const free = now;
+        now = next;
+        next = after;
+        after = free;
+    }
+}
+
+// ---- even shares ------------------------------------------------------------------------------
+// Tiles of sequences of any lengths, weighed in stages, laid end to end and cut into as many equal runs as there are workgroups: a run
+// is the end of a tile, whole tiles and the beginning of another.  What does not cover its tile is left as a part, and the parts of a tile are added in their order.
+struct PlanTile {
+    int64_t before;                             // stages in front of it
+    int32_t q0, nq, k0, nk, first, stages;
+};
+struct Plan {
+    int64_t stages;                             // of a head
+    int64_t tiles;
+    PlanTile tile[1];                           // tiles + 1 of them
+};
+constexpr int kLeast = 4;                       // stages: a run has that many, and no cut lies nearer to the edge of a tile
+
+struct Runs {
+    const HOPL_GLOBAL Plan* plan;
+    int64_t all;                                // stages of all heads
+    int64_t blocks;
+    __device__ __forceinline__ Runs(const void* p, int heads, int most) : plan((const HOPL_GLOBAL Plan*)p) {
+        all = plan->stages * heads;
+        blocks = all / kLeast;
+        blocks = blocks < 1 ? 1 : blocks > most ? most : blocks;
+    }
+};
+__device__ __forceinline__ PlanTile tile_of(const Runs& r, int64_t number) {
+    const HOPL_GLOBAL PlanTile* t = &r.plan->tile[number];
+    auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return {t->before, same(t->q0), same(t->nq), same(t->k0), same(t->nk), same(t->first), same(t->stages)};
+}
+struct Place {
+    int64_t tile;                               // head * tiles + number
+    int stage;
+};
+// Where the run of workgroup `block` begins: the same for all wavefronts, which search 64 tiles at a time.
+__device__ __forceinline__ Place begin_of_run(const Runs& r, int64_t block) {
+    const int64_t tiles = r.plan->tiles;
+    const int64_t w = block * r.all / r.blocks;
+    if (!r.all || w >= r.all) return {r.all / (r.plan->stages ? r.plan->stages : 1) * tiles, 0};
+    const int64_t head = w / r.plan->stages, in = w - head * r.plan->stages;
+    int64_t low = 0, high = tiles;              // tile[low].before <= in < tile[high].before
+    while (high - low > 1) {
+        const int64_t step = (high - low + 63) / 64, at = low + (threadIdx.x & 63) * step;
+        const uint64_t before = __ballot(at < high && r.plan->tile[at].before <= in);
+        low += (63 - __builtin_clzll(before)) * step;
+        high = low + step < high ? low + step : high;
+    }
+    const int stage = (int)(in - r.plan->tile[low].before), stages = r.plan->tile[low].stages;
+    if (stage < kLeast) return {head * tiles + low, 0};
+    if (stages - stage < kLeast) return {head * tiles + low + 1, 0};
+    return {head * tiles + low, stage};
+}
+// The workgroups whose runs begin inside of a tile, from *first to *last; false: none does.
+__device__ __forceinline__ bool runs_inside(const Runs& r, int64_t head, const PlanTile& tile, int64_t* first, int64_t* last) {
+    if (tile.stages < 2 * kLeast) return false;
+    const int64_t from = head * r.plan->stages + tile.before + kLeast, to = head * r.plan->stages + tile.before + tile.stages - kLeast + 1;    // [from, to)
+    *first = (from * r.blocks + r.all - 1) / r.all;
+    *last = (to * r.blocks + r.all - 1) / r.all - 1;
+    return *first <= *last;
+}
 
 }  // namespace hopa

@@ -27,6 +27,13 @@ struct HopAttentionTask {
     void *dq, *dk, *dv;
     int64_t lddq, lddk, lddv;
     float* terms;                          // of every pair, [2][k_heads][q_rows group]: lse log2(e) and sum do o
+    void *q_plan, *k_plan;                 // how pairs and keys are shared out
+};
+
+// What the gradient needs besides its terms: most tiles of pairs and keys, and bytes of their plans and of the parts that wait to be joined.
+struct HopAttentionPlan {
+    int64_t q_tiles, k_tiles;
+    size_t q_bytes, k_bytes, partial_bytes;
 };
 
 struct HopRotateTask {
@@ -48,10 +55,9 @@ struct HopRotateTask {
 };
 
 int hopa_forward_parts(const HopAttentionTask& t, int dtype);
-int hopa_dq_parts(const HopAttentionTask& t, int dtype);
-int hopa_dkv_parts(const HopAttentionTask& t, int dtype);
 int hopa_forward(const HopAttentionTask& t, int dtype, void* stream);
-int hopa_grad(const HopAttentionTask& t, int dtype, int dq_parts, int dkv_parts, void* stream);
+HopAttentionPlan hopa_grad_plan(const HopAttentionTask& t, int dtype);
+int hopa_grad(const HopAttentionTask& t, int dtype, const HopAttentionPlan& plan, void* stream);
 
 int hopa_rotate(const HopRotateTask& t, int dtype, const HopIndex& index, void* stream);
 int hopa_rotate_grad(const HopRotateTask& t, int dtype, const HopIndex& index, const HopIndex& dindex, void* stream);
