@@ -98,7 +98,15 @@ bool attention_grads_ok(const hop_attention_args* a, const hop_attention_grads* 
         return false;
     return a->k_rows == 0 || (heads_ok(g->dk, g->lddk, narrow, e) && heads_ok(g->dv, g->lddv, narrow, e));
 }
-size_t term_bytes(const hop_attention_args* a) { return ((size_t)2 * a->q_heads * a->q_rows * 4 + 255) / 256 * 256; }
+HopAttentionTask gradient_task(const hop_attention_args* a, const hop_attention_grads* g) {
+    HopAttentionTask t = attention_task(a);
+    t.grad = g->grad; t.ldgrad = g->ldgrad;
+    t.o = const_cast<void*>(g->o); t.ldo = g->ldo;
+    t.lse = const_cast<float*>(g->lse);
+    t.dq = g->dq; t.dk = g->dk; t.dv = g->dv;
+    t.lddq = g->lddq; t.lddk = g->lddk; t.lddv = g->lddv;
+    return t;
+}
 
 }  // namespace
 
@@ -168,27 +176,17 @@ int hop_attention(const hop_attention_args* a, void* o, int64_t ldo, float* lse,
 
 size_t hop_attention_grad_scratch_bytes(const hop_attention_args* a, const hop_attention_grads* g) {
     if (!attention_grads_ok(a, g) || (a->q_rows == 0 && a->k_rows == 0)) return 0;
-    const HopAttentionPlan p = hopa_grad_plan(attention_task(a), a->dtype);
-    return term_bytes(a) + p.q_bytes + p.k_bytes + p.partial_bytes;
+    HopAttentionTask t = gradient_task(a, g);
+    return hopa_grad_plan(&t, a->dtype, nullptr).bytes;
 }
 
 int hop_attention_grad(const hop_attention_args* a, const hop_attention_grads* g, void* scratch, size_t scratch_bytes, void* stream) {
     if (!attention_grads_ok(a, g)) return HOP_ERR_INVALID_ARG;
     if (a->q_rows == 0 && a->k_rows == 0) return HOP_OK;
-    if (scratch_bytes < hop_attention_grad_scratch_bytes(a, g)) return HOP_ERR_ARENA_TOO_SMALL;
+    HopAttentionTask t = gradient_task(a, g);
+    const HopAttentionPlan p = hopa_grad_plan(&t, a->dtype, (char*)scratch);
+    if (scratch_bytes < p.bytes) return HOP_ERR_ARENA_TOO_SMALL;
     if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
-    HopAttentionTask t = attention_task(a);
-    t.grad = g->grad; t.ldgrad = g->ldgrad;
-    t.o = const_cast<void*>(g->o); t.ldo = g->ldo;
-    t.lse = const_cast<float*>(g->lse);
-    t.dq = g->dq; t.dk = g->dk; t.dv = g->dv;
-    t.lddq = g->lddq; t.lddk = g->lddk; t.lddv = g->lddv;
-    const HopAttentionPlan p = hopa_grad_plan(t, a->dtype);
-    char* at = (char*)scratch;
-    t.terms = (float*)at;
-    t.q_plan = at += term_bytes(a);
-    t.k_plan = at += p.q_bytes;
-    t.partial = (float*)(at + p.k_bytes);
     const int rc = hopa_grad(t, a->dtype, p, stream);
     return rc ? hip_fail((hipError_t)rc, "attention gradient launch") : HOP_OK;
 }

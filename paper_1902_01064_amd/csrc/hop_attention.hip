@@ -66,6 +66,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 
         feed_v.put(sv);
     };
 
+    const Places<T, D> places;
     f32x16 o[kU];
     float top, sum;                            // of scores in powers of two; over the lane's own half of the column
     auto clear = [&]() __attribute__((always_inline)) {
@@ -78,13 +79,14 @@ __global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 
     // registers for other things (a prompt of 8192 rows: 235 us, one by one 203).
     auto units = [&](auto n, const char* sk, const char* sv, int key) __attribute__((always_inline)) {
         constexpr int N = decltype(n)::value;
+        const Places<T, D> at = places;
         f32x16 p[N];
 #pragma unroll
         for (int u = 0; u < N; ++u) p[u] = (f32x16)(0.f);
 #pragma unroll
         for (int i = 0; i < L::kSteps; ++i)
 #pragma unroll
-            for (int u = 0; u < N; ++u) p[u] = multiply(L::along(sk, 32 * u, i), fq[i], p[u]);
+            for (int u = 0; u < N; ++u) p[u] = multiply(L::along(sk + 32 * u * L::kLine, at.along, i), fq[i], p[u]);
         if (key + 32 * N > all_see) {
             asm volatile("");                  // a branch, which few tiles take, and not selections that all of them make
 #pragma unroll
@@ -121,9 +123,9 @@ __global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const Weights<T> w(p[u]);
-            Sums<T, D, false> sums;
-            sums.begin(sv + 32 * u * L::kLine, sv);
-            sums.add(sv + 32 * u * L::kLine, sv, w, w, o, o);
+            Sums<T, D> sums;
+            sums.begin(sv + 32 * u * L::kLine, at.across);
+            sums.add(sv + 32 * u * L::kLine, at.across, w, o);
         }
     };
     auto turn = [&](const char* sk, const char* sv, int key) __attribute__((always_inline)) {
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 
                 put(sk0, sv0);
                 arrive();
                 if (key + kRows > all_see_here) {
-                    add_not_finite<T, D>(sv0, min(kRows, seq.nk - key), o, [&](int j) { return key + j < limit; });
+                    add_not_finite<T, D, D>(sv0, 0, 0, min(kRows, seq.nk - key), o, [&](int j) { return key + j < limit; });
                     __syncthreads();
                     drop_not_finite<T, kBytes, NT>(sv0);
                     __syncthreads();

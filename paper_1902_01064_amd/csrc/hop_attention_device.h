@@ -5,6 +5,8 @@
 // second operand of the product that contracts over those rows: softmax and its gradient never leave the registers.
 #pragma once
 
+#include <type_traits>
+
 #include "hop_attention_internal.h"
 #include "hop_layers_device.h"
 
@@ -35,11 +37,12 @@ struct Tile {
         return ((r & 3) << 2) | (r >> 2 & 3);
     }
     // The first operand of a product over columns: lane l holds row l % 32, chunk 2 step + l / 32.  Places are a number of the lane's, with a constant's bits flipped,
-    // and a constant behind it, so that few registers hold the addresses of all reads.
-    static __device__ __forceinline__ frag along(const char* s, int row0, int step) {
-        const int lane = threadIdx.x & 63, row = lane & 31, place = row * kLine + (((lane >> 5) ^ swizzle(row)) << 4);
-        return *(const frag*)(s + (place ^ (step * 32)) + row0 * kLine);
+    // and a constant behind it, so that one register holds the addresses of all reads.
+    static __device__ __forceinline__ int along_place() {
+        const int lane = threadIdx.x & 63, row = lane & 31;
+        return row * kLine + (((lane >> 5) ^ swizzle(row)) << 4);
     }
+    static __device__ __forceinline__ frag along(const char* s, int place, int step) { return *(const frag*)(s + (place ^ (step * 32))); }
 };
 
 __device__ __forceinline__ f32x16 multiply(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -49,7 +52,7 @@ __device__ __forceinline__ f32x16 multiply(f32x4 a, f32x4 b, f32x16 c) {
     return c;
 }
 
-// An accumulator as the second operand of a product over its rows: two parts of 16 rows.  `across` reads the first operand, of a tile's rows from row0 on and 32 columns.
+// An accumulator as the second operand of a product over its rows: two parts of 16 rows.  `across` reads the first operand, 16 of a tile's rows and 32 columns.
 // bf16: part u holds rows 16 u + 4 (lane / 32) + e and, from element 4 on, 8 more; the transposing read brings the tile's in the same order (16 lanes hold
 // four rows of 16 columns each, lane l of them gets column l).  fp32: an element to a product.
 template <typename T>
@@ -58,21 +61,28 @@ template <>
 struct Weights<bf16> {
     typedef bf16x8 Part;
     Part part[2];
+    static __device__ __forceinline__ Part part_of(const f32x16& p, int u) {
+        Part r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = (bf16)p[8 * u + e];               // to nearest, ties to even
+        return r;
+    }
     __device__ __forceinline__ explicit Weights(const f32x16& p) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) part[u][e] = (bf16)p[8 * u + e];     // to nearest, ties to even
+        part[0] = part_of(p, 0);
+        part[1] = part_of(p, 1);
     }
     template <int D>
-    static __device__ __forceinline__ Part across(const char* s, int row0, int unit, int u) {
+    static __device__ __forceinline__ int across_place() {
         typedef Tile<bf16, D> L;
         const int lane = threadIdx.x & 63, row = 4 * (lane >> 5) + (lane >> 2 & 3);
-        const int place = row * L::kLine + (((lane >> 4 & 1) * 2 + (lane >> 1 & 1) ^ L::swizzle(row)) << 4) + (lane & 1) * 8;
+        return row * L::kLine + (((lane >> 4 & 1) * 2 + (lane >> 1 & 1) ^ L::swizzle(row)) << 4) + (lane & 1) * 8;
+    }
+    template <int D>
+    static __device__ __forceinline__ Part across(const char* s, int place, int unit, int u) {
         union { s16x4 half[2]; bf16x8 all; } a;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const char* at = s + (place ^ (unit * 64 + h * 32)) + (row0 + 16 * u + 8 * h) * L::kLine;
+            const char* at = s + (place ^ (unit * 64 + h * 32)) + (16 * u + 8 * h) * Tile<bf16, D>::kLine;
             a.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
         }
         return a.all;
@@ -83,17 +93,26 @@ template <>
 struct Weights<float> {
     typedef f32x8 Part;
     Part part[2];
-    __device__ __forceinline__ explicit Weights(const f32x16& p) {
+    static __device__ __forceinline__ Part part_of(const f32x16& p, int u) {
+        Part r;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) part[e >> 3][e & 7] = p[e];
+        for (int e = 0; e < 8; ++e) r[e] = p[8 * u + e];
+        return r;
+    }
+    __device__ __forceinline__ explicit Weights(const f32x16& p) {
+        part[0] = part_of(p, 0);
+        part[1] = part_of(p, 1);
     }
     template <int D>
-    static __device__ __forceinline__ Part across(const char* s, int row0, int unit, int u) {
-        typedef Tile<float, D> L;
-        const int lane = threadIdx.x & 63, hi = lane >> 5, place = 4 * hi * L::kLine + (((lane & 31) >> 2 ^ hi << 3) << 4) + (lane & 3) * 4;
+    static __device__ __forceinline__ int across_place() {
+        const int lane = threadIdx.x & 63, hi = lane >> 5;
+        return 4 * hi * Tile<float, D>::kLine + (((lane & 31) >> 2 ^ hi << 3) << 4) + (lane & 3) * 4;
+    }
+    template <int D>
+    static __device__ __forceinline__ Part across(const char* s, int place, int unit, int u) {
         Part a;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) a[r] = *(const float*)(s + (place ^ (unit * 128 + r * 16)) + (row0 + 16 * u + 8 * (r >> 2) + (r & 3)) * L::kLine);
+        for (int r = 0; r < 8; ++r) a[r] = *(const float*)(s + (place ^ (unit * 128 + r * 16)) + (16 * u + 8 * (r >> 2) + (r & 3)) * Tile<float, D>::kLine);
         return a;
     }
     static __device__ __forceinline__ f32x16 add(const Part& a, const Part& b, f32x16 c) {
@@ -103,69 +122,48 @@ struct Weights<float> {
     }
 };
 
+// Places of operands, worked out again for every unit: held over a loop they would fill the registers.
+template <typename T, int D>
+struct Places {
+    int along = Tile<T, D>::along_place(), across = Weights<T>::template across_place<D>();
+    __device__ __forceinline__ Places again() const {
+        Places p = *this;
+        asm volatile("" : "+v"(p.along), "+v"(p.across));
+        return p;
+    }
+};
+
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void static_for(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        static_for<N, I + 1>(f);
+    }
+}
+
 // ---- products in turn with other things -----------------------------------------------------
 // Left to itself the compiler reads an operand right in front of the product that wants it, so that every product waits for LDS, and puts all arithmetic behind
 // all products.  Here the order is written down: operands are read kAhead products early, and between two of them the matrix unit has a share of other work beside it.
 //
-// Scores of 32 rows of one or two tiles with the columns c0 (c1): beside(e) is called for e = 0 .. 15 in between.
-template <typename T, int D, bool TWO, typename BESIDE>
-__device__ __forceinline__ void scores_beside(const char* s0, const char* s1, const typename Tile<T, D>::frag* c0, const typename Tile<T, D>::frag* c1, f32x16& r0, f32x16& r1,
-                                              BESIDE beside) {
-    typedef Tile<T, D> L;
-    constexpr int kN = L::kSteps, kAhead = sizeof(T) == 4 ? 2 : 4;
-    typename L::frag a0[kAhead], a1[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-        a0[i] = L::along(s0, 0, i);
-        if constexpr (TWO) a1[i] = L::along(s1, 0, i);
-    }
-    r0 = (f32x16)(0.f);
-    if constexpr (TWO) r1 = (f32x16)(0.f);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-        r0 = multiply(a0[i % kAhead], c0[i], r0);
-        if constexpr (TWO) r1 = multiply(a1[i % kAhead], c1[i], r1);
-        if (i + kAhead < kN) {
-            a0[i % kAhead] = L::along(s0, 0, i + kAhead);
-            if constexpr (TWO) a1[i % kAhead] = L::along(s1, 0, i + kAhead);
-        }
-#pragma unroll
-        for (int e = i * 16 / kN; e < (i + 1) * 16 / kN; ++e) beside(e);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-}
-
-// c0[column][.] += sum over 32 rows of tile s0 times w0, and the same of c1, s1, w1.  `begin` reads the first operands.
-template <typename T, int D, bool TWO>
+// sum[column][.] += sum over 32 rows of a tile times w.  `begin` reads the first operands.
+template <typename T, int D>
 struct Sums {
     typedef Weights<T> W;
-    static constexpr int kU = D / 32, kN = kU * (TWO ? 4 : 2), kAhead = sizeof(T) == 4 ? 2 : kN < 6 ? kN : 6;
+    static constexpr int kU = D / 32, kN = kU * 2, kAhead = sizeof(T) == 4 ? 2 : kN < 6 ? kN : 6;
     typename W::Part a[kAhead];
-    // Products in an order in which neighbours have different sums: both tiles', or two columns'.
-    static __device__ __forceinline__ void item(int k, int* which, int* unit, int* u) {
-        *which = TWO ? k & 1 : 0;
-        *u = k >> 1 & 1;
-        *unit = TWO ? k >> 2 : (k >> 2) * 2 + (k & 1);
-    }
-    static __device__ __forceinline__ typename W::Part read(const char* s0, const char* s1, int k) {
-        int which, unit, u;
-        item(k, &which, &unit, &u);
-        return W::template across<D>(which ? s1 : s0, 0, unit, u);
-    }
-    __device__ __forceinline__ void begin(const char* s0, const char* s1) {
+    // Products in an order in which neighbours have different sums.
+    static __device__ __forceinline__ typename W::Part read(const char* s, int place, int k) { return W::template across<D>(s, place, (k >> 2) * 2 + (k & 1), k >> 1 & 1); }
+    __device__ __forceinline__ void begin(const char* s, int place) {
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) a[k] = read(s0, s1, k);
+        for (int k = 0; k < kAhead; ++k) a[k] = read(s, place, k);
     }
-    __device__ __forceinline__ void add(const char* s0, const char* s1, const W& w0, const W& w1, f32x16* c0, f32x16* c1) {
+    __device__ __forceinline__ void add(const char* s, int place, const W& w, f32x16* sum) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
-            int which, unit, u;
-            item(k, &which, &unit, &u);
-            f32x16& c = which ? c1[unit] : c0[unit];
-            c = W::add(a[k % kAhead], (which ? w1 : w0).part[u], c);
-            if (k + kAhead < kN) a[k % kAhead] = read(s0, s1, k + kAhead);
+            f32x16& c = sum[(k >> 2) * 2 + (k & 1)];
+            c = W::add(a[k % kAhead], w.part[k >> 1 & 1], c);
+            if (k + kAhead < kN) a[k % kAhead] = read(s, place, k + kAhead);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -322,18 +320,18 @@ __device__ __forceinline__ bool all_finite(const f32x16 (&acc)[N]) {
         for (int e = 0; e < 16; ++e) fine = fine && __builtin_fabsf(acc[t][e]) < kInf;
     return fine;
 }
-// seen(j): whether the lane's column sees row j of the tile
-template <typename T, int D, typename SEEN>
-__device__ __forceinline__ void add_not_finite(const char* s, int count, f32x16 (&acc)[D / 32], SEEN seen) {
+// COLS columns from `column` on, of rows from `from` to `count`; seen(j): whether the lane's column sees row j of the tile
+template <typename T, int D, int COLS, typename SEEN>
+__device__ __forceinline__ void add_not_finite(const char* s, int column, int from, int count, f32x16 (&acc)[COLS / 32], SEEN seen) {
     typedef Tile<T, D> L;
     const int hi = (threadIdx.x & 63) >> 5;
-    for (int j = 0; j < count; ++j) {
+    for (int j = from; j < count; ++j) {
         const bool here = seen(j);
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
+        for (int t = 0; t < COLS / 32; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int c = 32 * t + 8 * (e >> 2) + 4 * hi + (e & 3);
+                const int c = column + 32 * t + 8 * (e >> 2) + 4 * hi + (e & 3);
                 const float v = (float)*(const T*)(s + j * L::kLine + (((c / L::kChunk) ^ L::swizzle(j)) << 4) + c % L::kChunk * sizeof(T));
                 acc[t][e] += here && !(__builtin_fabsf(v) < kInf) ? v : 0.f;
             }
@@ -443,43 +441,26 @@ __device__ __forceinline__ Sequence sequence(const HopAttentionTask& t, int s) {
 __device__ __forceinline__ int visible(const Sequence& q, int causal, int row) { return causal ? clamp_int(row + 1 + q.nk - q.nq, 0, q.nk) : q.nk; }
 
 
-// ---- a pipeline over stages -----------------------------------------------------------------
-// n stages of U units through three buffers, one barrier a stage: while a stage is worked on, the next one has arrived or is on its way, and every
-// step starts the products of the unit that follows (`step(i, buffer, unit, buffer of the next unit, next unit)`) beside the arithmetic of its own, which
-// otherwise would wait for one another within a wavefront.  The unit behind the last one is whatever lies in LDS; nobody uses its scores.
-// The buffers are three restricted pointers, so that the compiler knows that reads of one need not wait for loads into another.
-template <int U, typename ISSUE, typename FIRST, typename STEP>
-__device__ __forceinline__ void pipeline_begin(char* __restrict now, char* __restrict next, int n, ISSUE issue, FIRST first, STEP step) {
-    if (n > 1) issue(next, 1);
-    first(now);
-#pragma unroll
-    for (int u = 0; u + 1 < U; ++u) step(0, now, u, now, u + 1);
+// ---- stages -----------------------------------------------------------------------------------
+// n stages through two buffers, one barrier a stage: the next one is on its way while a stage is worked on.  The buffers are two restricted pointers, so that the
+// compiler knows that reads of one need not wait for loads into the other.
+template <typename ISSUE, typename WORK>
+__device__ __forceinline__ void stage(char* __restrict now, char* __restrict next, int i, int n, ISSUE issue, WORK work) {
+    if (i + 1 < n) issue(next, i + 1);
+    work(now, i);
 }
-// The last unit of a stage and all but the last of the next one.
-template <int U, typename ISSUE, typename PUT, typename STEP>
-__device__ __forceinline__ void pipeline_turn(char* __restrict now, char* __restrict next, char* __restrict after, int i, int n, ISSUE issue, PUT put, STEP step) {
-    if (i + 1 < n) put(next);
-    arrive();                                   // the next stage is there, and nobody reads from the one before this any more
-    if (i + 2 < n) issue(after, i + 2);
-    step(i, now, U - 1, next, 0);
-    if (i + 1 < n)
-#pragma unroll
-        for (int u = 0; u + 1 < U; ++u) step(i + 1, next, u, next, u + 1);
-}
-template <int U, typename ISSUE, typename PUT, typename FIRST, typename STEP>
-__device__ __forceinline__ void pipeline(int n, char* pool, int bytes, ISSUE issue, PUT put, FIRST first, STEP step) {
-    char *now = pool, *next = pool + bytes, *after = pool + 2 * bytes;
+template <typename ISSUE, typename PUT, typename WORK>
+__device__ __forceinline__ void stages(int n, char* pool, int bytes, ISSUE issue, PUT put, WORK work) {
+    char *now = pool, *next = pool + bytes;
     __syncthreads();                            // with whoever still reads from the buffers
     issue(now, 0);
-    put(now);
-    arrive();
-    pipeline_begin<U>(now, next, n, issue, first, step);
     for (int i = 0; i < n; ++i) {
-        pipeline_turn<U>(now, next, after, i, n, issue, put, step);
-        char* const free = now;
+        put(now);
+        arrive();                               // this stage is there, and nobody reads from the one before any more
+        stage(now, next, i, n, issue, work);
+        char* const other = now;
         now = next;
-        next = after;
-        after = free;
+        next = other;
     }
 }
 

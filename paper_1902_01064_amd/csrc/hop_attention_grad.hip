@@ -15,13 +15,12 @@ using namespace hopa;
 
 namespace {
 
-template <typename T, int D>
-constexpr int kTileRows = D * (int)sizeof(T) <= 256 ? 64 : 32;
-constexpr int kShift = 7, kTile = 1 << kShift;          // pairs or keys of a tile
-// Workgroups on a CU at once: registers and LDS of one with 128 columns or fp32 leave no room for another.
-template <typename T, int D>
-constexpr int kBeside = sizeof(T) == 2 && D <= 64 ? 2 : 1;
+constexpr int kShift = 7, kTile = 1 << kShift;          // pairs or keys of a tile, 32 of a wavefront
 constexpr int kCus = 256;
+// Two halves of a workgroup with the same tile take every other 32 rows of a stage, so that a SIMD has two wavefronts, of which one computes while the other waits, and the CU
+// only one set of tiles.  In fp32 with 128 columns the sums and operands of one wavefront fill a SIMD's registers.
+template <typename T, int D>
+constexpr int kHalves = D * (int)sizeof(T) <= 256 ? 2 : 1;
 
 __device__ __forceinline__ int64_t pairs_of(const HopAttentionTask& t) { return (int64_t)t.q_rows * t.group; }
 // The first pair that sees a key.
@@ -117,14 +116,36 @@ __device__ __forceinline__ float* part_place(const HopAttentionTask& t, int64_t 
     return t.partial + (block * 2 + (first_part ? 1 : 0)) * sums * kTile * t.cols;
 }
 
+// The second half's sums, added to the first one's.
+template <int N, int HALVES>
+__device__ __forceinline__ void add_halves(char* pool, int half, int wave, f32x16 (&sum)[N]) {
+    if constexpr (HALVES == 2) {
+        float* mine = (float*)pool + wave * N * 16 * 64 + (threadIdx.x & 63);
+        __syncthreads();
+        if (half)
+#pragma unroll
+            for (int c = 0; c < N; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mine[(c * 16 + e) * 64] = sum[c][e];
+        __syncthreads();
+        if (!half)
+#pragma unroll
+            for (int c = 0; c < N; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[c][e] += mine[(c * 16 + e) * 64];
+    }
+}
+
 // ---- dq ---------------------------------------------------------------------------------
-template <typename T, int D, bool FED>
-__global__ __launch_bounds__(256, (kBeside<T, D>)) void attention_dq_kernel(HopAttentionTask t) {
+template <typename T, int D>
+__global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attention_dq_kernel(HopAttentionTask t) {
     typedef Tile<T, D> L;
-    constexpr int NT = 256, kRows = kTileRows<T, D>, kBytes = kRows * L::kLine, kU = D / 32;
+    typedef Weights<T> W;
+    constexpr int kH = kHalves<T, D>, NT = 256 * kH, kRows = 32 * kH, kBytes = kRows * L::kLine, kU = D / 32, kS = L::kSteps;
     constexpr int kStage = 2 * kBytes;                      // keys, values
-    __shared__ __attribute__((aligned(16))) char pool[3 * kStage];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hi = lane >> 5;
+    __shared__ __attribute__((aligned(16))) char pool[2 * kStage];
+    const int half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3), lane = threadIdx.x & 63, hi = lane >> 5;
+    const Places<T, D> all_places;
     const Runs runs(t.q_plan, t.k_heads, gridDim.x);
     const int64_t block = run_of_block(runs.blocks);
     if (block >= runs.blocks) return;
@@ -140,25 +161,25 @@ __global__ __launch_bounds__(256, (kBeside<T, D>)) void attention_dq_kernel(HopA
         const bool live = pair < pairs;
         const int row = live ? divide(pair, t.group_inverse) : 0, its = live ? pair - row * t.group : 0;
         const int64_t at = seq.q0 + row;
-        const int column = (head * t.group + its) * t.cols;
-        const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.cols;
-        const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.cols;
+        const int column = (head * t.group + its) * t.cols, from_column = (head * t.group + its) * t.head;
+        const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.head;
+        const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.head;
 
-        typename L::frag fq[L::kSteps], fg[L::kSteps];
-        load_columns<T, D, FED>(fq, (const T*)t.q + at * t.ldq + column, t.cols, live);
-        load_columns<T, D, FED>(fg, (const T*)t.grad + at * t.ldgrad + column, t.cols, live);
+        typename L::frag fq[kS], fg[kS];
+        load_columns<T, D, true>(fq, (const T*)t.q + at * t.ldq + from_column, t.head, live);
+        load_columns<T, D, true>(fg, (const T*)t.grad + at * t.ldgrad + from_column, t.head, live);
         float delta = 0.f;
         {
-            typename L::frag fo[L::kSteps];
-            load_columns<T, D, FED>(fo, (const T*)t.o + at * t.ldo + column, t.cols, live);
+            typename L::frag fo[kS];
+            load_columns<T, D, true>(fo, (const T*)t.o + at * t.ldo + from_column, t.head, live);
 #pragma unroll
-            for (int i = 0; i < L::kSteps; ++i)
+            for (int i = 0; i < kS; ++i)
 #pragma unroll
                 for (int e = 0; e < L::kChunk; ++e) delta = __builtin_fmaf((float)fo[i][e], (float)fg[i][e], delta);
         }
         delta = both_sum(delta);
         const float lse = live ? ((const HOPL_GLOBAL float*)t.lse)[(int64_t)(head * t.group + its) * t.q_rows + at] * (1.f / kLn2) : 0.f;
-        if (live && !hi && first_stage == 0) {
+        if (live && !hi && !half && first_stage == 0) {
             HOPL_GLOBAL float* terms = (HOPL_GLOBAL float*)t.terms + head * pairs_of(t) + (int64_t)seq.q0 * t.group + pair;
             terms[0] = lse;
             terms[t.k_heads * pairs_of(t)] = delta;
@@ -168,8 +189,8 @@ __global__ __launch_bounds__(256, (kBeside<T, D>)) void attention_dq_kernel(HopA
         const int all_see = visible_of(min(mine, pairs - 1)), all_see_here = visible_of(first);
         const int end = min(visible_of(min(first + kTile, pairs) - 1), last_stage * kRows), begin = first_stage * kRows;
 
-        const Rows gk = {t.ldk, 1, 0, t.cols}, gv = {t.ldv, 1, 0, t.cols};
-        Feed<T, D, kRows, NT, FED, false> feed_k, feed_v;
+        const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
+        Feed<T, D, kRows, NT, true, false> feed_k, feed_v;
         feed_k.begin(gk, 0);
         feed_v.begin(gv, 0);
         auto issue = [&](char* b, int i) __attribute__((always_inline)) {
@@ -177,59 +198,83 @@ __global__ __launch_bounds__(256, (kBeside<T, D>)) void attention_dq_kernel(HopA
             feed_k.issue(b, k, gk, key, seq.nk - key);
             feed_v.issue(b + kBytes, v, gv, key, seq.nk - key);
         };
-        auto put = [&](char* b) __attribute__((always_inline)) {
-            feed_k.put(b);
-            feed_v.put(b + kBytes);
-        };
-        f32x16 dq[kU], p, ds;
-        // the scores of the unit at `next` (or none), beside a unit's own gradients of scores and what they add
-        auto step = [&](const char* b, int key, const char* next) __attribute__((always_inline)) {
-            f32x16 next_p, next_ds;
-            scores_beside<T, D, true>(next, next + kBytes, fq, fg, next_p, next_ds,
-                                      [&](int r) __attribute__((always_inline)) { ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], t.scale_log2, -lse)) * (ds[r] - delta); });
-            Sums<T, D, false> sums;
-            sums.begin(b, b);
+        f32x16 dq[kU];
+        // Scores; do v^T beside their exponentials; sums of the first 16 keys beside the second 16's gradients, then of those.
+        auto work = [&](const char* b, int i) __attribute__((always_inline)) {
+            const Places<T, D> places = all_places.again();
+            const int key = begin + i * kRows + 32 * half;
+            const char* sk = b + 32 * half * L::kLine;
+            const char* sv = sk + kBytes;
+            constexpr int kN = 2 * kS + 2 * kU, kAhead = sizeof(T) == 4 ? 2 : 4, kFrom = kS + (sizeof(T) == 4 ? 1 : 2);
+            typename L::frag a[kAhead];
+            typename W::Part c[kAhead];
+            auto fetch = [&](auto n) __attribute__((always_inline)) {
+                constexpr int j = decltype(n)::value;
+                if constexpr (j < kS) a[j % kAhead] = L::along(sk, places.along, j);
+                else if constexpr (j < 2 * kS) a[j % kAhead] = L::along(sv, places.along, j - kS);
+                else if constexpr (j < kN) c[j % kAhead] = W::template across<D>(sk, places.across, (j - 2 * kS) % kU, (j - 2 * kS) / kU);
+            };
+            f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
+            static_for<kAhead>([&](auto n) __attribute__((always_inline)) { fetch(n); });
+            static_for<2 * kS>([&](auto n) __attribute__((always_inline)) {
+                constexpr int j = decltype(n)::value;
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (j < kS) p = multiply(a[j % kAhead], fq[j], p);
+                else ds = multiply(a[j % kAhead], fg[j - kS], ds);
+                fetch(std::integral_constant<int, j + kAhead>());
+                if constexpr (j >= kFrom)
+#pragma unroll
+                    for (int r = (j - kFrom) * 16 / (2 * kS - kFrom); r < (j - kFrom + 1) * 16 / (2 * kS - kFrom); ++r)
+                        p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], t.scale_log2, -lse));
+            });
+            __builtin_amdgcn_sched_barrier(0);
+            float less = delta;
             if (key + 32 > all_see) {
                 asm volatile("");              // a branch, which few tiles take, and not selections that all of them make
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (key + 8 * (r >> 2) + 4 * hi + (r & 3) >= limit) ds[r] = 0.f;
+                for (int r = 0; r < 16; ++r) {
+                    ds[r] = key + 8 * (r >> 2) + 4 * hi + (r & 3) < limit ? p[r] * (ds[r] - delta) : 0.f;
+                    p[r] = 1.f;
+                }
+                less = 0.f;
             }
-            const Weights<T> w(ds);
-            sums.add(b, b, w, w, dq, dq);
-            p = next_p;
-            ds = next_ds;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) ds[r] = p[r] * (ds[r] - less);
+            static_for<2 * kU>([&](auto n) __attribute__((always_inline)) {
+                constexpr int j = decltype(n)::value;
+                dq[j % kU] = W::add(c[(j + 2 * kS) % kAhead], W::part_of(ds, j / kU), dq[j % kU]);
+                fetch(std::integral_constant<int, j + 2 * kS + kAhead>());
+                if constexpr (j < kU)
+#pragma unroll
+                    for (int r = 8 + j * 8 / kU; r < 8 + (j + 1) * 8 / kU; ++r) ds[r] = p[r] * (ds[r] - less);
+                __builtin_amdgcn_sched_barrier(0);
+            });
         };
-        auto scores = [&](const char* b) __attribute__((always_inline)) { scores_beside<T, D, true>(b, b + kBytes, fq, fg, p, ds, [](int) {}); };
         auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int c = 0; c < kU; ++c) dq[c] = (f32x16)(0.f);
         };
         clear();
-        if (begin < end)
-            pipeline<kRows / 32>((end - begin + kRows - 1) / kRows, pool, kStage, issue, put, scores, [&](int i, const char* b, int u, const char* next, int next_u) __attribute__((always_inline)) {
-                step(b + 32 * u * L::kLine, begin + i * kRows + 32 * u, next + 32 * next_u * L::kLine);
-            });
+        const int n = begin < end ? (end - begin + kRows - 1) / kRows : 0;
+        if (n) stages(n, pool, kStage, issue, [](char*) {}, work);
         if (t.causal && __syncthreads_or(live && !all_finite(dq))) {
             clear();
-            for (int key = begin; key < end; key += kRows) {
+            for (int i = 0; i < n; ++i) {
+                const int key = begin + i * kRows;
                 __syncthreads();
-                issue(pool, (key - begin) / kRows);
-                put(pool);
+                issue(pool, i);
                 arrive();
                 if (key + kRows > all_see_here) {
-                    add_not_finite<T, D>(pool, min(kRows, seq.nk - key), dq, [&](int j) { return key + j < limit; });
+                    add_not_finite<T, D, D>(pool, 0, 32 * half, min(32 * half + 32, seq.nk - key), dq, [&](int j) { return key + j < limit; });
                     __syncthreads();
                     drop_not_finite<T, kBytes, NT>(pool);
                     __syncthreads();
                 }
-                for (int u = 0; u < kRows / 32; ++u) {
-                    scores(pool + 32 * u * L::kLine);
-                    step(pool + 32 * u * L::kLine, key + 32 * u, pool);
-                }
+                work(pool, i);
             }
         }
-        if (!live) continue;
+        add_halves<kU, kH>(pool, half, wave, dq);
+        if (!live || half) continue;
         if (first_stage > 0 || last_stage < seq.stages)
             store_columns<float, D>(part_place(t, block, first_stage == 0, 1) + (int64_t)(pair - first) * t.cols, t.cols, dq, 1.f);
         else
@@ -238,13 +283,20 @@ __global__ __launch_bounds__(256, (kBeside<T, D>)) void attention_dq_kernel(HopA
 }
 
 // ---- dk and dv ------------------------------------------------------------------------------
-template <typename T, int D, bool FED>
-__global__ __launch_bounds__(256, (kBeside<T, D>)) void attention_dkv_kernel(HopAttentionTask t) {
+template <typename T, int D>
+__global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attention_dkv_kernel(HopAttentionTask t) {
     typedef Tile<T, D> L;
-    constexpr int NT = 256, kRows = kTileRows<T, D>, kBytes = kRows * L::kLine, kU = D / 32;
-    constexpr int kStage = 2 * kBytes + 512;                // queries, gradients, lse log2(e) of 64 pairs, their D
-    __shared__ __attribute__((aligned(16))) char pool[3 * kStage];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hi = lane >> 5;
+    typedef Weights<T> W;
+    constexpr int kH = kHalves<T, D>, NT = 256 * kH, kRows = 32 * kH, kBytes = kRows * L::kLine, kS = L::kSteps;
+    constexpr int kStage = 2 * kBytes + 512;                // queries, gradients, lse log2(e) of the pairs, their D
+    // Both sums of 128 columns leave no registers for the keys and values: there they wait in LDS.
+    constexpr bool kHeld = kH == 1 || D * sizeof(T) <= 128;
+    // In fp32 keys, values and both sums of 128 columns are more than all registers of a SIMD: the sums are made 64 columns at a time, each from scores of its own.
+    constexpr int kCuts = kH == 1 ? 2 : 1, kSumCols = D / kCuts, kU = kSumCols / 32;
+    __shared__ __attribute__((aligned(16))) char pool[2 * kStage], tile[kHeld ? 16 : 2 * kTile * L::kLine], zeros[128];
+    const int half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3), lane = threadIdx.x & 63, hi = lane >> 5;
+    if (threadIdx.x < 32) ((float*)zeros)[threadIdx.x] = 0.f;
+    const Places<T, D> all_places;
     const Runs runs(t.k_plan, t.k_heads, gridDim.x);
     const int64_t block = run_of_block(runs.blocks);
     if (block >= runs.blocks) return;
@@ -259,101 +311,164 @@ __global__ __launch_bounds__(256, (kBeside<T, D>)) void attention_dkv_kernel(Hop
         const bool live = key < seq.nk;
         const int64_t at = seq.k0 + (live ? key : 0);
         const int pairs = seq.nq * t.group;
-        const T* q = (const T*)t.q + seq.q0 * t.ldq + head * t.group * t.cols;
-        const T* g = (const T*)t.grad + seq.q0 * t.ldgrad + head * t.group * t.cols;
+        const T* q = (const T*)t.q + seq.q0 * t.ldq + head * t.group * t.head;
+        const T* g = (const T*)t.grad + seq.q0 * t.ldgrad + head * t.group * t.head;
         const float* terms = t.terms + head * pairs_of(t) + (int64_t)seq.q0 * t.group;
 
-        typename L::frag fk[L::kSteps], fv[L::kSteps];
-        load_columns<T, D, FED>(fk, (const T*)t.k + at * t.ldk + head * t.cols, t.cols, live);
-        load_columns<T, D, FED>(fv, (const T*)t.v + at * t.ldv + head * t.cols, t.cols, live);
+        const char* const keys = tile + 32 * wave * L::kLine;
+        const char* const values = keys + kTile * L::kLine;
+        typename L::frag fk[kHeld ? kS : 1], fv[kHeld ? kS : 1];
+        if constexpr (kHeld) {
+            load_columns<T, D, true>(fk, (const T*)t.k + at * t.ldk + head * t.head, t.head, live);
+            load_columns<T, D, true>(fv, (const T*)t.v + at * t.ldv + head * t.head, t.head, live);
+        } else {
+            const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
+            __syncthreads();                               // with whoever still reads the tile before
+            Feed<T, D, kTile, NT, true, false> feed;
+            feed.begin(gk, 0);
+            feed.issue(tile, (const T*)t.k + seq.k0 * t.ldk + head * t.head, gk, first, seq.nk - first);
+            feed.begin(gv, 0);
+            feed.issue(tile + kTile * L::kLine, (const T*)t.v + seq.k0 * t.ldv + head * t.head, gv, first, seq.nk - first);
+        }
         const int least = live ? seen_from(t, seq.nq, seq.nk, key) : 0;
         const int all_see = seen_from(t, seq.nq, seq.nk, min(mine + 32, seq.nk) - 1), all_see_here = seen_from(t, seq.nq, seq.nk, min(first + kTile, seq.nk) - 1);
         const int start = min(pairs, seen_from(t, seq.nq, seq.nk, first) / kRows * kRows);
         const int begin = start + first_stage * kRows, end = min(pairs, start + last_stage * kRows);
-        const Rows gq = {t.ldq, t.group, t.group_inverse, t.cols}, gg = {t.ldgrad, t.group, t.group_inverse, t.cols};
-        Feed<T, D, kRows, NT, FED, true> feed_q, feed_g;
+        const Rows gq = {t.ldq, t.group, t.group_inverse, t.head}, gg = {t.ldgrad, t.group, t.group_inverse, t.head};
+        Feed<T, D, kRows, NT, true, true> feed_q, feed_g;
         feed_q.begin(gq, 0);
         feed_g.begin(gg, 0);
         auto issue = [&](char* b, int i) __attribute__((always_inline)) {
             const int pair = begin + i * kRows;
             feed_q.issue(b, q, gq, pair, pairs - pair);
             feed_g.issue(b + kBytes, g, gg, pair, pairs - pair);
-            if (wave < 2) {
+            if (!half && wave < 2) {
                 const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(terms + wave * t.k_heads * pairs_of(t) + pair), 0,
                                                                                    min(kRows, pairs - pair) * 4, 0x00020000);
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(b + 2 * kBytes + wave * 256), 4, lane * 4, 0, 0, 0);
             }
         };
-        auto put = [&](char* b) __attribute__((always_inline)) {
-            feed_q.put(b);
-            feed_g.put(b + kBytes);
-        };
-        f32x16 dk[kU], dv[kU], p, ds;
-        auto step = [&](const char* b, const char* terms_of_unit, int pair, const char* next) __attribute__((always_inline)) {
-            f32x16 next_p, next_ds;
-            f32x4 lse[4], delta[4];
+        int cut = 0;
+        f32x16 dk[kU], dv[kU];
+        // Scores; do v^T beside their exponentials; dv's sums beside the gradients of the scores; dk's.
+        auto work = [&](const char* b, int i) __attribute__((always_inline)) {
+            Places<T, D> places = all_places.again();
+            if constexpr (kCuts > 1) places.across ^= cut * kSumCols * (int)sizeof(T);
+            const int pair = begin + i * kRows + 32 * half;
+            const char* sq = b + 32 * half * L::kLine;
+            const char* sg = sq + kBytes;
+            const char* st = b + 2 * kBytes + 128 * half + 16 * hi;
+            constexpr int kN = 2 * kS + 4 * kU, kAhead = sizeof(T) == 4 ? 2 : kHeld ? 4 : 3, kFrom = kS + (sizeof(T) == 4 ? 1 : 2);
+            typename L::frag a[kAhead], own[kHeld ? 1 : kAhead];
+            typename W::Part c[kAhead];
+            auto fetch = [&](auto n) __attribute__((always_inline)) {
+                constexpr int j = decltype(n)::value, m = j - 2 * kS;
+                if constexpr (j < kS) {
+                    a[j % kAhead] = L::along(sq, places.along, j);
+                    if constexpr (!kHeld) own[j % kAhead] = L::along(keys, places.along, j);
+                } else if constexpr (j < 2 * kS) {
+                    a[j % kAhead] = L::along(sg, places.along, j - kS);
+                    if constexpr (!kHeld) own[j % kAhead] = L::along(values, places.along, j - kS);
+                } else if constexpr (j < kN) {
+                    c[j % kAhead] = W::template across<D>(m < 2 * kU ? sg : sq, places.across, m % kU, m / kU % 2);
+                }
+            };
+            f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
+            f32x4 lse[2], delta[2];                // four pairs' are read while the four in front of them are worked on
+            lse[0] = *(const f32x4*)st;
+            static_for<kAhead>([&](auto n) __attribute__((always_inline)) { fetch(n); });
+            static_for<2 * kS>([&](auto n) __attribute__((always_inline)) {
+                constexpr int j = decltype(n)::value;
+                __builtin_amdgcn_sched_barrier(0);
+                auto column = [&](auto& held) __attribute__((always_inline)) {
+                    if constexpr (kHeld) return held[j % kS];
+                    else return own[j % kAhead];
+                };
+                if constexpr (j < kS) p = multiply(a[j % kAhead], column(fk), p);
+                else ds = multiply(a[j % kAhead], column(fv), ds);
+                fetch(std::integral_constant<int, j + kAhead>());
+                if constexpr (j >= kFrom)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                lse[i] = *(const f32x4*)(terms_of_unit + 32 * i + 16 * hi);
-                delta[i] = *(const f32x4*)(terms_of_unit + 256 + 32 * i + 16 * hi);
-            }
-            scores_beside<T, D, true>(next, next + kBytes, fk, fv, next_p, next_ds, [&](int r) __attribute__((always_inline)) {
-                p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], t.scale_log2, -lse[r >> 2][r & 3]));
-                ds[r] = p[r] * (ds[r] - delta[r >> 2][r & 3]);
+                    for (int r = (j - kFrom) * 16 / (2 * kS - kFrom); r < (j - kFrom + 1) * 16 / (2 * kS - kFrom); ++r) {
+                        if (r % 4 == 0 && r < 12) lse[(r / 4 + 1) % 2] = *(const f32x4*)(st + 32 * (r / 4 + 1));
+                        p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], t.scale_log2, -lse[r / 4 % 2][r % 4]));
+                    }
             });
-            Sums<T, D, true> sums;
-            sums.begin(b + kBytes, b);
+            __builtin_amdgcn_sched_barrier(0);
+            W wp(p);
+            const char* sd = st + 256;
             if (pair < all_see) {
                 asm volatile("");              // a branch, as above
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (pair + 8 * (r >> 2) + 4 * hi + (r & 3) < least) p[r] = ds[r] = 0.f;
+                for (int r = 0; r < 16; ++r) {
+                    const bool here = pair + 8 * (r >> 2) + 4 * hi + (r & 3) >= least;
+                    ds[r] = here ? p[r] * (ds[r] - *(const float*)(sd + 32 * (r >> 2) + 4 * (r & 3))) : 0.f;
+                    p[r] = here ? p[r] : 0.f;
+                }
+                wp = W(p);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = 1.f;           // what follows leaves ds as it is
+                sd = zeros + 16 * hi;
             }
-            const Weights<T> wp(p), ws(ds);
-            sums.add(b + kBytes, b, wp, ws, dv, dk);
-            p = next_p;
-            ds = next_ds;
+            delta[0] = *(const f32x4*)sd;
+            static_for<2 * kU>([&](auto n) __attribute__((always_inline)) {
+                constexpr int j = decltype(n)::value;
+                dv[j % kU] = W::add(c[(j + 2 * kS) % kAhead], wp.part[j / kU], dv[j % kU]);
+                fetch(std::integral_constant<int, j + 2 * kS + kAhead>());
+#pragma unroll
+                for (int r = j * 8 / kU; r < (j + 1) * 8 / kU; ++r) {
+                    if (r % 4 == 0 && r < 12) delta[(r / 4 + 1) % 2] = *(const f32x4*)(sd + 32 * (r / 4 + 1));
+                    ds[r] = p[r] * (ds[r] - delta[r / 4 % 2][r % 4]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            const W ws(ds);
+            static_for<2 * kU>([&](auto n) __attribute__((always_inline)) {
+                constexpr int j = decltype(n)::value;
+                dk[j % kU] = W::add(c[(j + 2 * kS + 2 * kU) % kAhead], ws.part[j / kU], dk[j % kU]);
+                fetch(std::integral_constant<int, j + 2 * kS + 2 * kU + kAhead>());
+                __builtin_amdgcn_sched_barrier(0);
+            });
         };
-        auto scores = [&](const char* b) __attribute__((always_inline)) { scores_beside<T, D, true>(b, b + kBytes, fk, fv, p, ds, [](int) {}); };
         auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int c = 0; c < kU; ++c) dk[c] = dv[c] = (f32x16)(0.f);
         };
-        clear();
-        if (begin < end)
-            pipeline<kRows / 32>((end - begin + kRows - 1) / kRows, pool, kStage, issue, put, scores, [&](int i, const char* b, int u, const char* next, int next_u) __attribute__((always_inline)) {
-                step(b + 32 * u * L::kLine, b + 2 * kBytes + 128 * u, begin + i * kRows + 32 * u, next + 32 * next_u * L::kLine);
-            });
-        if (t.causal && __syncthreads_or(live && !(all_finite(dk) && all_finite(dv)))) {
+        const int n = begin < end ? (end - begin + kRows - 1) / kRows : 0;
+        for (; cut < kCuts; ++cut) {
             clear();
-            for (int pair = begin; pair < end; pair += kRows) {
-                __syncthreads();
-                issue(pool, (pair - begin) / kRows);
-                put(pool);
-                arrive();
-                if (pair < all_see_here) {
-                    const int count = min(kRows, pairs - pair);
-                    add_not_finite<T, D>(pool, count, dk, [&](int j) { return pair + j >= least; });
-                    add_not_finite<T, D>(pool + kBytes, count, dv, [&](int j) { return pair + j >= least; });
+            if (n) stages(n, pool, kStage, issue, [](char*) {}, work);
+            if (t.causal && __syncthreads_or(live && !(all_finite(dk) && all_finite(dv)))) {
+                clear();
+                for (int i = 0; i < n; ++i) {
+                    const int pair = begin + i * kRows;
                     __syncthreads();
-                    drop_not_finite<T, kBytes, NT>(pool);
-                    drop_not_finite<T, kBytes, NT>(pool + kBytes);
-                    __syncthreads();
-                }
-                for (int u = 0; u < kRows / 32; ++u) {
-                    scores(pool + 32 * u * L::kLine);
-                    step(pool + 32 * u * L::kLine, pool + 2 * kBytes + 128 * u, pair + 32 * u, pool);
+                    issue(pool, i);
+                    arrive();
+                    if (pair < all_see_here) {
+                        const int count = min(32 * half + 32, pairs - pair);
+                        add_not_finite<T, D, kSumCols>(pool, cut * kSumCols, 32 * half, count, dk, [&](int j) { return pair + j >= least; });
+                        add_not_finite<T, D, kSumCols>(pool + kBytes, cut * kSumCols, 32 * half, count, dv, [&](int j) { return pair + j >= least; });
+                        __syncthreads();
+                        drop_not_finite<T, kBytes, NT>(pool);
+                        drop_not_finite<T, kBytes, NT>(pool + kBytes);
+                        __syncthreads();
+                    }
+                    work(pool, i);
                 }
             }
-        }
-        if (!live) continue;
-        if (first_stage > 0 || last_stage < seq.stages) {
-            float* part = part_place(t, block, first_stage == 0, 2) + (int64_t)(key - first) * t.cols;
-            store_columns<float, D>(part, t.cols, dk, 1.f);
-            store_columns<float, D>(part + kTile * t.cols, t.cols, dv, 1.f);
-        } else {
-            store_columns<T, D>((T*)t.dk + at * t.lddk + head * t.cols, t.cols, dk, t.scale);
-            store_columns<T, D>((T*)t.dv + at * t.lddv + head * t.cols, t.cols, dv, 1.f);
+            add_halves<kU, kH>(pool, half, wave, dk);
+            add_halves<kU, kH>(pool, half, wave, dv);
+            const int column = cut * kSumCols, cols = t.cols - column;
+            if (!live || half || cols <= 0) continue;
+            if (first_stage > 0 || last_stage < seq.stages) {
+                float* part = part_place(t, block, first_stage == 0, 2) + (int64_t)(key - first) * t.cols;
+                store_columns<float, kSumCols>(part + column, cols, dk, 1.f);
+                store_columns<float, kSumCols>(part + kTile * t.cols + column, cols, dv, 1.f);
+            } else {
+                store_columns<T, kSumCols>((T*)t.dk + at * t.lddk + head * t.cols + column, cols, dk, t.scale);
+                store_columns<T, kSumCols>((T*)t.dv + at * t.lddv + head * t.cols + column, cols, dv, 1.f);
+            }
         }
     }
 }
@@ -391,42 +506,95 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTa
     }
 }
 
-template <typename T, int D, bool FED>
+// ---- rows that the memory unit cannot take, laid out anew -----------------------------------------
+// It fills tiles 16 bytes at a time, from addresses that are multiples of them.  Matrices whose rows or heads are not get a copy with heads of whole 16 bytes (zeros
+// at the end): read and written once, in one launch, beside two passes over them that follow.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_align_kernel(HopAttentionCopies c) {
+    typedef Tile<T, 64> L;                      // of which only the chunks matter
+    const auto& m = c.of[blockIdx.y];
+    const int chunks = c.head / L::kChunk, per_row = m.heads * chunks;
+    int b = 0, e = m.rows;
+    if (m.begin) {
+        b = clamp_int(((const HOPL_GLOBAL int32_t*)m.begin)[0], 0, m.rows);
+        e = clamp_int(((const HOPL_GLOBAL int32_t*)m.begin)[c.S], b, m.rows);
+    }
+    const int64_t all = (int64_t)(e - b) * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = b + i / per_row;
+        const int at = (int)(i % per_row), head = at / chunks, column = at % chunks * L::kChunk, n = c.cols - column;
+        const T* from = (const T*)m.from + row * m.ld + head * c.cols + column;
+        typename L::frag v;
+        if (n >= L::kChunk) v = *(const HOPL_GLOBAL typename L::frag_any*)from;
+        else v = load_short<typename L::frag>(from, n);
+        *(HOPL_GLOBAL typename L::frag*)((T*)m.to + row * m.heads * c.head + head * c.head + column) = v;
+    }
+}
+
+template <typename T, int D>
 int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t stream) {
-    const int grid = kCus * kBeside<T, D>;
-    constexpr int kJoins = kTile / 16;
-    attention_plan_kernel<<<dim3(2), dim3(kPlanners), 0, stream>>>(t, kTileRows<T, D>, plan.q_tiles, plan.k_tiles);
+    constexpr int grid = kCus, kThreads = 256 * kHalves<T, D>, kJoins = kTile / 16;
+    attention_plan_kernel<<<dim3(2), dim3(kPlanners), 0, stream>>>(t, 32 * kHalves<T, D>, plan.q_tiles, plan.k_tiles);
     if (t.q_rows) {
-        attention_dq_kernel<T, D, FED><<<dim3(grid), dim3(256), 0, stream>>>(t);
+        attention_dq_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
         (attention_grad_join_kernel<T, false>)<<<dim3((unsigned)(plan.q_tiles * t.k_heads * kJoins)), dim3(256), 0, stream>>>(t, grid);
     }
     if (t.k_rows) {
-        attention_dkv_kernel<T, D, FED><<<dim3(grid), dim3(256), 0, stream>>>(t);
+        attention_dkv_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
         (attention_grad_join_kernel<T, true>)<<<dim3((unsigned)(plan.k_tiles * t.k_heads * kJoins)), dim3(256), 0, stream>>>(t, grid);
     }
     return (int)hipGetLastError();
 }
 
 template <typename T>
-int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t stream) {
-    auto fits = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && (ld * sizeof(T)) % 16 == 0; };
-    const bool fed = fits(t.q, t.ldq) && fits(t.k, t.ldk) && fits(t.v, t.ldv) && fits(t.grad, t.ldgrad) && fits(t.o, t.ldo) && (t.cols * sizeof(T)) % 16 == 0;
-    if (t.cols <= 64) return fed ? launch<T, 64, true>(t, plan, stream) : launch<T, 64, false>(t, plan, stream);
-    return fed ? launch<T, 128, true>(t, plan, stream) : launch<T, 128, false>(t, plan, stream);
+int launch(HopAttentionTask t, const HopAttentionPlan& plan, hipStream_t stream) {
+    if (plan.copies.n) {
+        int64_t most = 1;
+        for (int i = 0; i < plan.copies.n; ++i)
+            most = std::max<int64_t>(most, ((int64_t)plan.copies.of[i].rows * plan.copies.of[i].heads * plan.copies.head * sizeof(T) / 16 + 255) / 256);
+        attention_align_kernel<T><<<dim3((unsigned)std::min<int64_t>(most, 2048), (unsigned)plan.copies.n), dim3(256), 0, stream>>>(plan.copies);
+    }
+    return t.cols <= 64 ? launch<T, 64>(t, plan, stream) : launch<T, 128>(t, plan, stream);
 }
 
 }  // namespace
 
-HopAttentionPlan hopa_grad_plan(const HopAttentionTask& t, int dtype) {
-    HopAttentionPlan p;
+HopAttentionPlan hopa_grad_plan(HopAttentionTask* task, int dtype, char* scratch) {
+    HopAttentionTask& t = *task;
+    HopAttentionPlan p = {};
     p.q_tiles = ((int64_t)t.q_rows * t.group + kTile - 1) / kTile + t.S;
     p.k_tiles = ((int64_t)t.k_rows + kTile - 1) / kTile + t.S;
-    auto bytes = [](int64_t tiles) { return (size_t)((sizeof(Plan) + tiles * sizeof(PlanTile) + 255) / 256 * 256); };
-    p.q_bytes = bytes(p.q_tiles);
-    p.k_bytes = bytes(p.k_tiles);
-    // two parts of a workgroup, dk and dv at most; fewer tiles than workgroups are cut only into as many
-    const int blocks = kCus * (dtype == HOP_BF16 && t.cols <= 64 ? 2 : 1);
-    p.partial_bytes = (size_t)blocks * 2 * 2 * kTile * t.cols * 4;
+    auto take = [&](size_t bytes) {
+        char* at = scratch + p.bytes;
+        p.bytes += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    auto plan_bytes = [](int64_t tiles) { return sizeof(Plan) + tiles * sizeof(PlanTile); };
+    t.terms = (float*)take((size_t)2 * t.k_heads * t.group * t.q_rows * 4);
+    t.q_plan = take(plan_bytes(p.q_tiles));
+    t.k_plan = take(plan_bytes(p.k_tiles));
+    t.partial = (float*)take((size_t)kCus * 2 * 2 * kTile * t.cols * 4);          // two parts of a workgroup, each of dk and dv
+    // copies of what the memory unit cannot take
+    const int elem = dtype == HOP_BF16 ? 2 : 4, chunk = 16 / elem, head = (t.cols + chunk - 1) / chunk * chunk;
+    auto fits = [&](const void* m, int64_t ld) { return ((uintptr_t)m & 15u) == 0 && (ld * elem) % 16 == 0; };
+    auto& c = p.copies;
+    t.head = head;
+    c.cols = t.cols;
+    c.head = head;
+    c.S = t.S;
+    auto align = [&](auto& m, int64_t& ld, int rows, int heads, const int32_t* begin) {
+        if (!rows || (head == t.cols && fits(m, ld))) return;
+        char* to = take((size_t)rows * heads * head * elem);
+        c.of[c.n++] = {m, to, ld, begin, rows, heads};
+        m = to;
+        ld = (int64_t)heads * head;
+    };
+    const int heads = t.k_heads * t.group;
+    align(t.q, t.ldq, t.q_rows, heads, t.q_begin);
+    align(t.grad, t.ldgrad, t.q_rows, heads, t.q_begin);
+    align(t.o, t.ldo, t.q_rows, heads, t.q_begin);
+    align(t.k, t.ldk, t.k_rows, t.k_heads, t.k_begin);
+    align(t.v, t.ldv, t.k_rows, t.k_heads, t.k_begin);
     return p;
 }
 

@@ -13,6 +13,7 @@ struct HopAttentionTask {
     const int32_t *q_begin, *k_begin;      // null: one sequence of all rows
     int32_t S, q_rows, k_rows;
     int32_t k_heads, group, cols;          // group: query heads of a key head
+    int32_t head;                          // gradient: columns from a head to the next one where q, k, v, o and grad are read
     uint32_t group_inverse;                // ceil(2^32 / group), 0 for 1
     int32_t causal, parts;
     float scale, scale_log2;               // scale_log2 = scale log2(e)
@@ -30,10 +31,22 @@ struct HopAttentionTask {
     void *q_plan, *k_plan;                 // how pairs and keys are shared out
 };
 
-// What the gradient needs besides its terms: most tiles of pairs and keys, and bytes of their plans and of the parts that wait to be joined.
+// Matrices that the gradient copies first, each to rows of `heads` heads `head` columns apart.
+struct HopAttentionCopies {
+    struct {
+        const void* from;
+        void* to;
+        int64_t ld;
+        const int32_t* begin;
+        int32_t rows, heads;
+    } of[5];
+    int32_t n, cols, head, S;
+};
+// What the gradient needs besides its task: most tiles of pairs and keys, copies to make, bytes of scratch.
 struct HopAttentionPlan {
     int64_t q_tiles, k_tiles;
-    size_t q_bytes, k_bytes, partial_bytes;
+    HopAttentionCopies copies;
+    size_t bytes;
 };
 
 struct HopRotateTask {
@@ -56,7 +69,7 @@ struct HopRotateTask {
 
 int hopa_forward_parts(const HopAttentionTask& t, int dtype);
 int hopa_forward(const HopAttentionTask& t, int dtype, void* stream);
-HopAttentionPlan hopa_grad_plan(const HopAttentionTask& t, int dtype);
+HopAttentionPlan hopa_grad_plan(HopAttentionTask* t, int dtype, char* scratch);           // sets t's parts of the scratch and what is read instead of its matrices
 int hopa_grad(const HopAttentionTask& t, int dtype, const HopAttentionPlan& plan, void* stream);
 
 int hopa_rotate(const HopRotateTask& t, int dtype, const HopIndex& index, void* stream);
