@@ -254,6 +254,13 @@ __device__ __forceinline__ void load_columns(typename Tile<T, D>::frag* to, cons
     }
 }
 
+// The same from a tile: a few loads of whole rows are far quicker than a load of every row's chunk by a lane of its own.
+template <typename T, int D>
+__device__ __forceinline__ void take_columns(typename Tile<T, D>::frag* to, const char* tile, int place) {
+#pragma unroll
+    for (int s = 0; s < Tile<T, D>::kSteps; ++s) to[s] = Tile<T, D>::along(tile, place, s);
+}
+
 __device__ __forceinline__ void store4(float* p, int n, f32x4 v) {
     if (n >= 4) {
         *(HOPL_GLOBAL f32x4_any*)p = v;
@@ -313,12 +320,12 @@ __device__ __forceinline__ float both_sum(float v) {
 // and sets it to zero in the tile before the matrix unit reads it.
 template <int N>
 __device__ __forceinline__ bool all_finite(const f32x16 (&acc)[N]) {
-    bool fine = true;
+    float nothing[4] = {0.f, 0.f, 0.f, 0.f};    // and NaN where it is not
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) fine = fine && __builtin_fabsf(acc[t][e]) < kInf;
-    return fine;
+        for (int e = 0; e < 16; ++e) nothing[e & 3] = __builtin_fmaf(acc[t][e], 0.f, nothing[e & 3]);
+    return (nothing[0] + nothing[1]) + (nothing[2] + nothing[3]) == 0.f;
 }
 // COLS columns from `column` on, of rows from `from` to `count`; seen(j): whether the lane's column sees row j of the tile
 template <typename T, int D, int COLS, typename SEEN>
@@ -449,11 +456,10 @@ __device__ __forceinline__ void stage(char* __restrict now, char* __restrict nex
     if (i + 1 < n) issue(next, i + 1);
     work(now, i);
 }
+// The first one is issued beforehand, behind a barrier with whoever still reads from the buffers.
 template <typename ISSUE, typename PUT, typename WORK>
 __device__ __forceinline__ void stages(int n, char* pool, int bytes, ISSUE issue, PUT put, WORK work) {
     char *now = pool, *next = pool + bytes;
-    __syncthreads();                            // with whoever still reads from the buffers
-    issue(now, 0);
     for (int i = 0; i < n; ++i) {
         put(now);
         arrive();                               // this stage is there, and nobody reads from the one before any more
@@ -465,25 +471,29 @@ __device__ __forceinline__ void stages(int n, char* pool, int bytes, ISSUE issue
 }
 
 // ---- even shares ------------------------------------------------------------------------------
-// Tiles of sequences of any lengths, weighed in stages, laid end to end and cut into as many equal runs as there are workgroups: a run
+// Tiles of sequences of any lengths, weighed in stages and what a tile takes beside them, laid end to end and cut into as many equal runs as there are workgroups: a run
 // is the end of a tile, whole tiles and the beginning of another.  What does not cover its tile is left as a part, and the parts of a tile are added in their order.
 struct PlanTile {
-    int64_t before;                             // stages in front of it
+    int64_t before;                             // weight in front of it
     int32_t q0, nq, k0, nk, first, stages;
 };
 struct Plan {
-    int64_t stages;                             // of a head
+    int64_t weight;                             // of a head's tiles
     int64_t tiles;
     PlanTile tile[1];                           // tiles + 1 of them
 };
 constexpr int kLeast = 4;                       // stages: a run has that many, and no cut lies nearer to the edge of a tile
+#ifndef KFIXED
+#define KFIXED 4
+#endif
+constexpr int kFixed = KFIXED;                       // stages that a tile's operands, its sums' way out and its part of the plan are worth
 
 struct Runs {
     const HOPL_GLOBAL Plan* plan;
-    int64_t all;                                // stages of all heads
+    int64_t all;                                // weight of all heads
     int64_t blocks;
     __device__ __forceinline__ Runs(const void* p, int heads, int most) : plan((const HOPL_GLOBAL Plan*)p) {
-        all = plan->stages * heads;
+        all = plan->weight * heads;
         blocks = all / kLeast;
         blocks = blocks < 1 ? 1 : blocks > most ? most : blocks;
     }
@@ -501,8 +511,8 @@ struct Place {
 __device__ __forceinline__ Place begin_of_run(const Runs& r, int64_t block) {
     const int64_t tiles = r.plan->tiles;
     const int64_t w = block * r.all / r.blocks;
-    if (!r.all || w >= r.all) return {r.all / (r.plan->stages ? r.plan->stages : 1) * tiles, 0};
-    const int64_t head = w / r.plan->stages, in = w - head * r.plan->stages;
+    if (!r.all || w >= r.all) return {r.all / (r.plan->weight ? r.plan->weight : 1) * tiles, 0};
+    const int64_t head = w / r.plan->weight, in = w - head * r.plan->weight;
     int64_t low = 0, high = tiles;              // tile[low].before <= in < tile[high].before
     while (high - low > 1) {
         const int64_t step = (high - low + 63) / 64, at = low + (threadIdx.x & 63) * step;
@@ -510,7 +520,7 @@ __device__ __forceinline__ Place begin_of_run(const Runs& r, int64_t block) {
         low += (63 - __builtin_clzll(before)) * step;
         high = low + step < high ? low + step : high;
     }
-    const int stage = (int)(in - r.plan->tile[low].before), stages = r.plan->tile[low].stages;
+    const int stage = (int)(in - r.plan->tile[low].before) - kFixed, stages = r.plan->tile[low].stages;
     if (stage < kLeast) return {head * tiles + low, 0};
     if (stages - stage < kLeast) return {head * tiles + low + 1, 0};
     return {head * tiles + low, stage};
@@ -518,7 +528,7 @@ __device__ __forceinline__ Place begin_of_run(const Runs& r, int64_t block) {
 // The workgroups whose runs begin inside of a tile, from *first to *last; false: none does.
 __device__ __forceinline__ bool runs_inside(const Runs& r, int64_t head, const PlanTile& tile, int64_t* first, int64_t* last) {
     if (tile.stages < 2 * kLeast) return false;
-    const int64_t from = head * r.plan->stages + tile.before + kLeast, to = head * r.plan->stages + tile.before + tile.stages - kLeast + 1;    // [from, to)
+    const int64_t at = head * r.plan->weight + tile.before + kFixed, from = at + kLeast, to = at + tile.stages - kLeast + 1;    // [from, to)
     *first = (from * r.blocks + r.all - 1) / r.all;
     *last = (to * r.blocks + r.all - 1) / r.all - 1;
     return *first <= *last;

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(kPlanners) void attention_plan_kernel(HopAttentionT
     }
     if (tiles > most) tiles = most;
     __syncthreads();
-    int64_t stages = 0;
+    int64_t weight = 0;
     for (int64_t base = 0; base < tiles; base += kPlanners) {
         const int64_t at = base + threadIdx.x;
         int64_t n = 0;
@@ -93,15 +93,15 @@ __global__ __launch_bounds__(kPlanners) void attention_plan_kernel(HopAttentionT
             tile.stages = (int32_t)n;
         }
         int64_t all;
-        tile.before = stages + scan_all(n, waves, &all);
+        tile.before = weight + scan_all(at < tiles ? n + kFixed : 0, waves, &all);
         if (at < tiles) plan->tile[at] = tile;
-        stages += all;
+        weight += all;
     }
     if (threadIdx.x == 0) {
         PlanTile end = {};
-        end.before = stages;
+        end.before = weight;
         plan->tile[tiles] = end;
-        plan->stages = stages;
+        plan->weight = weight;
         plan->tiles = tiles;
     }
 }
@@ -116,23 +116,26 @@ __device__ __forceinline__ float* part_place(const HopAttentionTask& t, int64_t 
     return t.partial + (block * 2 + (first_part ? 1 : 0)) * sums * kTile * t.cols;
 }
 
-// The second half's sums, added to the first one's.
+// The second half's sums, added to the first one's.  Nobody uses the pool any more.
 template <int N, int HALVES>
 __device__ __forceinline__ void add_halves(char* pool, int half, int wave, f32x16 (&sum)[N]) {
     if constexpr (HALVES == 2) {
-        float* mine = (float*)pool + wave * N * 16 * 64 + (threadIdx.x & 63);
-        __syncthreads();
+        char* mine = pool + (wave * N * 4 * 64 + (threadIdx.x & 63)) * 16;
         if (half)
 #pragma unroll
             for (int c = 0; c < N; ++c)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) mine[(c * 16 + e) * 64] = sum[c][e];
+                for (int e = 0; e < 4; ++e) *(f32x4*)(mine + (c * 4 + e) * 1024) = {sum[c][4 * e], sum[c][4 * e + 1], sum[c][4 * e + 2], sum[c][4 * e + 3]};
         __syncthreads();
         if (!half)
 #pragma unroll
             for (int c = 0; c < N; ++c)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum[c][e] += mine[(c * 16 + e) * 64];
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 more = *(const f32x4*)(mine + (c * 4 + e) * 1024);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[c][4 * e + i] += more[i];
+                }
     }
 }
 
@@ -144,6 +147,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
     constexpr int kH = kHalves<T, D>, NT = 256 * kH, kRows = 32 * kH, kBytes = kRows * L::kLine, kU = D / 32, kS = L::kSteps;
     constexpr int kStage = 2 * kBytes;                      // keys, values
     __shared__ __attribute__((aligned(16))) char pool[2 * kStage];
+    __shared__ int not_finite;
     const int half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3), lane = threadIdx.x & 63, hi = lane >> 5;
     const Places<T, D> all_places;
     const Runs runs(t.q_plan, t.k_heads, gridDim.x);
@@ -161,29 +165,10 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         const bool live = pair < pairs;
         const int row = live ? divide(pair, t.group_inverse) : 0, its = live ? pair - row * t.group : 0;
         const int64_t at = seq.q0 + row;
-        const int column = (head * t.group + its) * t.cols, from_column = (head * t.group + its) * t.head;
+        const int column = (head * t.group + its) * t.cols;
         const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.head;
         const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.head;
 
-        typename L::frag fq[kS], fg[kS];
-        load_columns<T, D, true>(fq, (const T*)t.q + at * t.ldq + from_column, t.head, live);
-        load_columns<T, D, true>(fg, (const T*)t.grad + at * t.ldgrad + from_column, t.head, live);
-        float delta = 0.f;
-        {
-            typename L::frag fo[kS];
-            load_columns<T, D, true>(fo, (const T*)t.o + at * t.ldo + from_column, t.head, live);
-#pragma unroll
-            for (int i = 0; i < kS; ++i)
-#pragma unroll
-                for (int e = 0; e < L::kChunk; ++e) delta = __builtin_fmaf((float)fo[i][e], (float)fg[i][e], delta);
-        }
-        delta = both_sum(delta);
-        const float lse = live ? ((const HOPL_GLOBAL float*)t.lse)[(int64_t)(head * t.group + its) * t.q_rows + at] * (1.f / kLn2) : 0.f;
-        if (live && !hi && !half && first_stage == 0) {
-            HOPL_GLOBAL float* terms = (HOPL_GLOBAL float*)t.terms + head * pairs_of(t) + (int64_t)seq.q0 * t.group + pair;
-            terms[0] = lse;
-            terms[t.k_heads * pairs_of(t)] = delta;
-        }
         const int limit = live ? visible(its_rows, t.causal, row) : seq.nk;
         auto visible_of = [&](int p) { return visible(its_rows, t.causal, divide(p, t.group_inverse)); };
         const int all_see = visible_of(min(mine, pairs - 1)), all_see_here = visible_of(first);
@@ -198,6 +183,51 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             feed_k.issue(b, k, gk, key, seq.nk - key);
             feed_v.issue(b + kBytes, v, gv, key, seq.nk - key);
         };
+        const int n = begin < end ? (end - begin + kRows - 1) / kRows : 0;
+        // The tile's queries, gradients and results come through the buffers of the stages.
+        const Rows gq = {t.ldq, t.group, t.group_inverse, t.head}, gg = {t.ldgrad, t.group, t.group_inverse, t.head}, go = {t.ldo, t.group, t.group_inverse, t.head};
+        Feed<T, D, kTile, NT, true, true> feed;
+        typename L::frag fq[kS], fg[kS];
+        char* const second = kH == 2 ? pool + kStage : pool;
+        const int in_tile = 32 * wave * L::kLine;
+        auto fetch_tile = [&](char* to, const void* m, const Rows& g) __attribute__((always_inline)) {
+            feed.begin(g, first - divide(first, t.group_inverse) * t.group);
+            feed.issue(to, (const T*)m + seq.q0 * g.ld + head * t.group * t.head, g, first, pairs - first);
+        };
+        __syncthreads();                                   // with whoever still reads from the buffers
+        if (threadIdx.x == 0) not_finite = 0;
+        fetch_tile(pool, t.q, gq);
+        if (kH == 2) fetch_tile(second, t.grad, gg);
+        arrive();
+        take_columns<T, D>(fq, pool + in_tile, all_places.along);
+        if (kH == 1) {
+            arrive();
+            fetch_tile(second, t.grad, gg);
+            arrive();
+        }
+        take_columns<T, D>(fg, second + in_tile, all_places.along);
+        arrive();
+        fetch_tile(second, t.o, go);
+        if (kH == 2 && n) issue(pool, 0);
+        const float lse = live ? ((const HOPL_GLOBAL float*)t.lse)[(int64_t)(head * t.group + its) * t.q_rows + at] * (1.f / kLn2) : 0.f;
+        arrive();
+        float delta = 0.f;
+#pragma unroll
+        for (int i = 0; i < kS; ++i) {
+            const typename L::frag fo = L::along(second + in_tile, all_places.along, i);
+#pragma unroll
+            for (int e = 0; e < L::kChunk; ++e) delta = __builtin_fmaf((float)fo[e], (float)fg[i][e], delta);
+        }
+        if (kH == 1) {
+            arrive();
+            if (n) issue(pool, 0);
+        }
+        delta = both_sum(delta);
+        if (live && !hi && !half && first_stage == 0) {
+            HOPL_GLOBAL float* terms = (HOPL_GLOBAL float*)t.terms + head * pairs_of(t) + (int64_t)seq.q0 * t.group + pair;
+            terms[0] = lse;
+            terms[t.k_heads * pairs_of(t)] = delta;
+        }
         f32x16 dq[kU];
         // Scores; do v^T beside their exponentials; sums of the first 16 keys beside the second 16's gradients, then of those.
         auto work = [&](const char* b, int i) __attribute__((always_inline)) {
@@ -255,9 +285,11 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             for (int c = 0; c < kU; ++c) dq[c] = (f32x16)(0.f);
         };
         clear();
-        const int n = begin < end ? (end - begin + kRows - 1) / kRows : 0;
         if (n) stages(n, pool, kStage, issue, [](char*) {}, work);
-        if (t.causal && __syncthreads_or(live && !all_finite(dq))) {
+        if (!n) __syncthreads();                           // the stages have theirs
+        if (t.causal && live && !all_finite(dq)) not_finite = 1;
+        __syncthreads();
+        if (not_finite) {
             clear();
             for (int i = 0; i < n; ++i) {
                 const int key = begin + i * kRows;
@@ -272,6 +304,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
                 }
                 work(pool, i);
             }
+            __syncthreads();
         }
         add_halves<kU, kH>(pool, half, wave, dq);
         if (!live || half) continue;
@@ -294,6 +327,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
     // In fp32 keys, values and both sums of 128 columns are more than all registers of a SIMD: the sums are made 64 columns at a time, each from scores of its own.
     constexpr int kCuts = kH == 1 ? 2 : 1, kSumCols = D / kCuts, kU = kSumCols / 32;
     __shared__ __attribute__((aligned(16))) char pool[2 * kStage], tile[kHeld ? 16 : 2 * kTile * L::kLine], zeros[128];
+    __shared__ int not_finite;
     const int half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3), lane = threadIdx.x & 63, hi = lane >> 5;
     if (threadIdx.x < 32) ((float*)zeros)[threadIdx.x] = 0.f;
     const Places<T, D> all_places;
@@ -315,21 +349,6 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         const T* g = (const T*)t.grad + seq.q0 * t.ldgrad + head * t.group * t.head;
         const float* terms = t.terms + head * pairs_of(t) + (int64_t)seq.q0 * t.group;
 
-        const char* const keys = tile + 32 * wave * L::kLine;
-        const char* const values = keys + kTile * L::kLine;
-        typename L::frag fk[kHeld ? kS : 1], fv[kHeld ? kS : 1];
-        if constexpr (kHeld) {
-            load_columns<T, D, true>(fk, (const T*)t.k + at * t.ldk + head * t.head, t.head, live);
-            load_columns<T, D, true>(fv, (const T*)t.v + at * t.ldv + head * t.head, t.head, live);
-        } else {
-            const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
-            __syncthreads();                               // with whoever still reads the tile before
-            Feed<T, D, kTile, NT, true, false> feed;
-            feed.begin(gk, 0);
-            feed.issue(tile, (const T*)t.k + seq.k0 * t.ldk + head * t.head, gk, first, seq.nk - first);
-            feed.begin(gv, 0);
-            feed.issue(tile + kTile * L::kLine, (const T*)t.v + seq.k0 * t.ldv + head * t.head, gv, first, seq.nk - first);
-        }
         const int least = live ? seen_from(t, seq.nq, seq.nk, key) : 0;
         const int all_see = seen_from(t, seq.nq, seq.nk, min(mine + 32, seq.nk) - 1), all_see_here = seen_from(t, seq.nq, seq.nk, min(first + kTile, seq.nk) - 1);
         const int start = min(pairs, seen_from(t, seq.nq, seq.nk, first) / kRows * kRows);
@@ -348,6 +367,36 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(b + 2 * kBytes + wave * 256), 4, lane * 4, 0, 0, 0);
             }
         };
+        const int n = begin < end ? (end - begin + kRows - 1) / kRows : 0;
+        const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
+        Feed<T, D, kTile, NT, true, false> feed;
+        auto fetch_tile = [&](char* to, const void* m, const Rows& g) __attribute__((always_inline)) {
+            feed.begin(g, 0);
+            feed.issue(to, (const T*)m + seq.k0 * g.ld + head * t.head, g, first, seq.nk - first);
+        };
+        const int in_tile = 32 * wave * L::kLine;
+        const char *const keys = tile + in_tile, *const values = keys + kTile * L::kLine;
+        typename L::frag fk[kHeld ? kS : 1], fv[kHeld ? kS : 1];
+        __syncthreads();                                   // with whoever still reads from the buffers
+        if (threadIdx.x == 0) not_finite = 0;
+        if constexpr (kHeld) {                             // through the buffers of the stages
+            char* const second = kH == 2 ? pool + kStage : pool;
+            fetch_tile(pool, t.k, gk);
+            if (kH == 2) fetch_tile(second, t.v, gv);
+            arrive();
+            take_columns<T, D>(fk, pool + in_tile, all_places.along);
+            if (kH == 1) {
+                arrive();
+                fetch_tile(second, t.v, gv);
+                arrive();
+            }
+            take_columns<T, D>(fv, second + in_tile, all_places.along);
+            arrive();
+        } else {
+            fetch_tile(tile, t.k, gk);
+            fetch_tile(tile + kTile * L::kLine, t.v, gv);
+        }
+        if (n) issue(pool, 0);
         int cut = 0;
         f32x16 dk[kU], dv[kU];
         // Scores; do v^T beside their exponentials; dv's sums beside the gradients of the scores; dk's.
@@ -434,11 +483,17 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
 #pragma unroll
             for (int c = 0; c < kU; ++c) dk[c] = dv[c] = (f32x16)(0.f);
         };
-        const int n = begin < end ? (end - begin + kRows - 1) / kRows : 0;
         for (; cut < kCuts; ++cut) {
+            if (cut) {
+                __syncthreads();
+                if (n) issue(pool, 0);
+            }
             clear();
             if (n) stages(n, pool, kStage, issue, [](char*) {}, work);
-            if (t.causal && __syncthreads_or(live && !(all_finite(dk) && all_finite(dv)))) {
+            if (!n) __syncthreads();                       // the stages have theirs
+            if (t.causal && live && !(all_finite(dk) && all_finite(dv))) not_finite = 1;
+            __syncthreads();
+            if (not_finite) {
                 clear();
                 for (int i = 0; i < n; ++i) {
                     const int pair = begin + i * kRows;
@@ -456,8 +511,10 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
                     }
                     work(pool, i);
                 }
+                __syncthreads();
             }
             add_halves<kU, kH>(pool, half, wave, dk);
+            if (kH == 2) __syncthreads();
             add_halves<kU, kH>(pool, half, wave, dv);
             const int column = cut * kSumCols, cols = t.cols - column;
             if (!live || half || cols <= 0) continue;
