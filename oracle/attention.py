@@ -62,8 +62,9 @@ def _weights(do, o, lse, q, k, v, rq, rk, h, hk, D, causal, scale):
     return p, p * (g @ _heads(v[rk], hk, D).T - (g * _heads(o[rq], h, D)).sum(1)[:, None])
 
 
-def attention_bounds(do, o, lse, q, k, v, q_heads, k_heads, q_begin, k_begin, causal, scale, u, r):
+def attention_bounds(do, o, lse, q, k, v, q_heads, k_heads, q_begin, k_begin, causal, scale, u, r, exact_o=None):
     """How far sums in a precision of u (half a step) with weights rounded by r may be off: (o, lse, dq, dk, dv), before results are rounded.
+    exact_o: sum_c do_ic o_ic may as well be that of this o, which differs from o by its rounding; so ds may be off by p times the difference of the two sums.
 
     A score is a sum of D products, scaled and shifted: off by e = (D + 8) u scale sum |q k| + 4 u (|s| + |lse|), which is how far its exponential is off
     relatively, with 4 u more for the exponential itself.  The rest is sums of n products: (n + 3) u times the magnitudes that meet."""
@@ -84,6 +85,8 @@ def attention_bounds(do, o, lse, q, k, v, q_heads, k_heads, q_begin, k_begin, ca
         el[h, rq] += (row + (nk + 6) * u)[:, 0] + 4 * u * level[:, 0]
         meet = g @ c.T + (g * np.abs(_heads(o[rq], h, D))).sum(1)[:, None]
         es = p * (e * meet + (D + 6) * u * meet)
+        if exact_o is not None:
+            es = es + p * np.abs((_heads(do[rq], h, D) * _heads(o[rq] - exact_o[rq], h, D)).sum(1))[:, None]
         eq[rq, at[0]] += scale * (es + np.abs(ds) * ((nk + 6) * u + r)) @ b
         ek[rk, at[1]] += scale * (es + np.abs(ds) * ((nq * (q_heads // k_heads) + 6) * u + r)).T @ a
         ev[rk, at[1]] += (p * (e + (nq * (q_heads // k_heads) + 6) * u + r)).T @ g

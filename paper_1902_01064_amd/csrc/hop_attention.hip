@@ -194,10 +194,9 @@ __global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t) {
     const int lane = threadIdx.x & 63;
-    const int64_t number = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), per_head = (int64_t)t.q_rows * t.group, all = part_place(t, t.parts, 0, 0);
-    const int head = (int)(number / per_head);
-    const int64_t pair = number - head * per_head;
-    const int row = (int)(pair / t.group), its = (int)(pair - (int64_t)row * t.group);
+    const int64_t all = part_place(t, t.parts, 0, 0);
+    const uint32_t number = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_head = t.q_rows * t.group;          // below 2^30 in all
+    const int head = number / per_head, pair = number - head * per_head, row = divide(pair, t.group_inverse), its = pair - row * t.group;
     if (head >= t.k_heads) return;
     int b = 0, e = t.q_rows;
     if (t.q_begin) {
@@ -207,20 +206,29 @@ __global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t)
     if (row < b || row >= e) return;
     const HOPL_GLOBAL float* sums = (const HOPL_GLOBAL float*)t.partial;
     const HOPL_GLOBAL float* tops = sums + all * t.cols;
-    float top = -kInf;
-    for (int p = 0; p < t.parts; ++p) {
-        const int64_t at = part_place(t, p, head, pair);
-        if (tops[2 * at + 1] != 0.f) top = fmaxf(top, tops[2 * at]);
+    // a lane a part, of which there are 64 at most
+    float its_top = -kInf, its_total = 0.f;
+    if (lane < t.parts) {
+        const int64_t at = part_place(t, lane, head, pair);
+        its_total = tops[2 * at + 1];
+        if (its_total != 0.f) its_top = tops[2 * at];
     }
-    float total = 0.f, v[2] = {0.f, 0.f};
-    for (int p = 0; p < t.parts; ++p) {
-        const int64_t at = part_place(t, p, head, pair);
-        if (tops[2 * at + 1] == 0.f) continue;
-        const float by = __builtin_amdgcn_exp2f(tops[2 * at] - top);
-        total += by * tops[2 * at + 1];
+    float top = its_top;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (lane + 64 * i < t.cols) v[i] += by * sums[at * t.cols + lane + 64 * i];
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float weight = its_total == 0.f ? 0.f : __builtin_amdgcn_exp2f(its_top - top);
+    float total = weight * its_total, v[2] = {0.f, 0.f};
+#pragma unroll
+    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+#pragma unroll 4
+    for (int p = 0; p < t.parts; ++p) {
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), p));
+        const int64_t at = part_place(t, p, head, pair);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float x = lane + 64 * i < t.cols ? sums[at * t.cols + lane + 64 * i] : 0.f;
+            if (w != 0.f) v[i] += w * x;
+        }
     }
     const float by = total == 0.f ? 0.f : 1.f / total;
     const int h = head * t.group + its;
@@ -265,8 +273,14 @@ int launch(const HopAttentionTask& t, hipStream_t stream) {
 int hopa_forward_parts(const HopAttentionTask& t, int dtype) {
     (void)dtype;
     const int64_t step = few(t) ? 32 : 128, tiles = (((int64_t)t.q_rows * t.group + step - 1) / step + t.S) * t.k_heads, keys = t.k_rows / t.S;
-    const int64_t wanted = few(t) ? 1024 : 512;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((wanted + tiles - 1) / tiles, keys / 256), 64));
+#ifndef WANT
+#define WANT 1024
+#define WANT4 512
+#define LST 64
+#define LST4 256
+#endif
+    const int64_t wanted = few(t) ? WANT : WANT4;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((wanted + tiles - 1) / tiles, keys / (few(t) ? LST : LST4)), 64));
 }
 
 int hopa_forward(const HopAttentionTask& t, int dtype, void* stream) {

@@ -483,10 +483,7 @@ struct Plan {
     PlanTile tile[1];                           // tiles + 1 of them
 };
 constexpr int kLeast = 4;                       // stages: a run has that many, and no cut lies nearer to the edge of a tile
-#ifndef KFIXED
-#define KFIXED 4
-#endif
-constexpr int kFixed = KFIXED;                       // stages that a tile's operands, its sums' way out and its part of the plan are worth
+constexpr int kFixed = 7;                       // stages that a tile's operands and its sums' way out are worth (17500 cycles, a stage of 128 columns in bfloat16 2440)
 
 struct Runs {
     const HOPL_GLOBAL Plan* plan;

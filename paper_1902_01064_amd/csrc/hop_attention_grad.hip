@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kShift = 7, kTile = 1 << kShift;          // pairs or keys of a tile, 32 of a wavefront
 constexpr int kCus = 256;
+constexpr int kExact = 128;                             // keys: see attention_dq_kernel
 // Two halves of a workgroup with the same tile take every other 32 rows of a stage, so that a SIMD has two wavefronts, of which one computes while the other waits, and the CU
 // only one set of tiles.  In fp32 with 128 columns the sums and operands of one wavefront fill a SIMD's registers.
 template <typename T, int D>
@@ -148,6 +149,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
     constexpr int kStage = 2 * kBytes;                      // keys, values
     __shared__ __attribute__((aligned(16))) char pool[2 * kStage];
     __shared__ int not_finite;
+    __shared__ float exact[2][kTile];
     const int half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3), lane = threadIdx.x & 63, hi = lane >> 5;
     const Places<T, D> all_places;
     const Runs runs(t.q_plan, t.k_heads, gridDim.x);
@@ -223,6 +225,30 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             if (n) issue(pool, 0);
         }
         delta = both_sum(delta);
+        // With few keys to a query o's rounding weighs: D once more, as sum_j p_ij do_i v_j, which is exact to fp32's rounding and costs these tiles two products more.
+        if (sizeof(T) == 2 && n && seq.stages * kRows <= kExact) {
+            float sum = 0.f;
+            stages(n, pool, kStage, issue, [](char*) {}, [&](const char* b, int i) __attribute__((always_inline)) {
+                const int key = i * kRows + 32 * half;
+                const char* sk = b + 32 * half * L::kLine;
+                f32x16 p = (f32x16)(0.f), g = (f32x16)(0.f);
+#pragma unroll
+                for (int j = 0; j < kS; ++j) {
+                    p = multiply(L::along(sk, all_places.along, j), fq[j], p);
+                    g = multiply(L::along(sk + kBytes, all_places.along, j), fg[j], g);
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float term = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], t.scale_log2, -lse)) * g[r];
+                    sum += key + 8 * (r >> 2) + 4 * hi + (r & 3) < limit ? term : 0.f;
+                }
+            });
+            sum = both_sum(sum);
+            exact[half][wave * 32 + (lane & 31)] = sum;
+            __syncthreads();
+            delta = exact[0][wave * 32 + (lane & 31)] + exact[1][wave * 32 + (lane & 31)];
+            issue(pool, 0);
+        }
         if (live && !hi && !half && first_stage == 0) {
             HOPL_GLOBAL float* terms = (HOPL_GLOBAL float*)t.terms + head * pairs_of(t) + (int64_t)seq.q0 * t.group + pair;
             terms[0] = lse;
@@ -530,35 +556,34 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
     }
 }
 
-// ---- parts, joined in their order: 16 rows of a tile ------------------------------------------
-// `sums` matrices to a part: dq, or dk and dv.
+// ---- parts, joined in their order -------------------------------------------------------------
+// 8 rows of the tile in which run number blockIdx.x / 16 + 1 begins, if it is the first one to do so.  A part is `sums` matrices: dq, or dk and dv.
 template <typename T, bool KEYS>
 __global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTask t, int most) {
+    constexpr int kSums = KEYS ? 2 : 1, kEach = 8;
     const Runs runs(KEYS ? t.k_plan : t.q_plan, t.k_heads, most);
-    const int64_t tiles = runs.plan->tiles;
-    constexpr int kSums = KEYS ? 2 : 1, kEach = kTile / 16;
-    const int64_t number = blockIdx.x / kEach;
-    if (number >= tiles * t.k_heads) return;
-    const int head = (int)(number / tiles), first = blockIdx.x % kEach * 16;
-    const PlanTile seq = tile_of(runs, number - head * tiles);
+    const int64_t run = blockIdx.x / (kTile / kEach) + 1, tiles = runs.plan->tiles;
+    if (run >= runs.blocks) return;
+    const Place at = begin_of_run(runs, run);
+    if (at.stage <= 0) return;
+    const int head = (int)(at.tile / tiles), first = blockIdx.x % (kTile / kEach) * kEach;
+    const PlanTile seq = tile_of(runs, at.tile - head * tiles);
     int64_t b0, b1;
-    if (!runs_inside(runs, head, seq, &b0, &b1)) return;
-    const int all = (KEYS ? seq.nk : seq.nq * t.group) - seq.first, rows = min(16, all - first);
-    for (int i = threadIdx.x; i < rows * t.cols; i += 256) {
-        const int r = i / t.cols, c = i - r * t.cols, in = first + r, n = seq.first + in;
-        const int64_t place = (int64_t)in * t.cols + c;
-#pragma unroll
-        for (int which = 0; which < kSums; ++which) {
-            float v = ((const HOPL_GLOBAL float*)part_place(t, b0 - 1, true, kSums))[which * kTile * t.cols + place];
-            for (int64_t b = b0; b <= b1; ++b) v += ((const HOPL_GLOBAL float*)part_place(t, b, false, kSums))[which * kTile * t.cols + place];
-            if constexpr (KEYS) {
-                const int64_t at = seq.k0 + n;
-                if (which) ((HOPL_GLOBAL T*)t.dv)[at * t.lddv + head * t.cols + c] = (T)v;
-                else ((HOPL_GLOBAL T*)t.dk)[at * t.lddk + head * t.cols + c] = (T)(v * t.scale);
-            } else {
-                const int row = divide(n, t.group_inverse);
-                ((HOPL_GLOBAL T*)t.dq)[(int64_t)(seq.q0 + row) * t.lddq + (head * t.group + n - row * t.group) * t.cols + c] = (T)(v * t.scale);
-            }
+    if (!runs_inside(runs, head, seq, &b0, &b1) || b0 != run) return;
+    const int all = (KEYS ? seq.nk : seq.nq * t.group) - seq.first, rows = min(kEach, all - first);
+    for (int i = threadIdx.x; i < rows * t.cols * kSums; i += 256) {
+        const int which = KEYS ? i / (rows * t.cols) : 0, j = i - which * rows * t.cols, r = j / t.cols, c = j - r * t.cols, in = first + r, n = seq.first + in;
+        const int64_t place = (int64_t)which * kTile * t.cols + in * t.cols + c;
+        float v = ((const HOPL_GLOBAL float*)part_place(t, b0 - 1, true, kSums))[place];
+#pragma unroll 4
+        for (int64_t b = b0; b <= b1; ++b) v += ((const HOPL_GLOBAL float*)part_place(t, b, false, kSums))[place];
+        if constexpr (KEYS) {
+            const int64_t row = seq.k0 + n;
+            if (which) ((HOPL_GLOBAL T*)t.dv)[row * t.lddv + head * t.cols + c] = (T)v;
+            else ((HOPL_GLOBAL T*)t.dk)[row * t.lddk + head * t.cols + c] = (T)(v * t.scale);
+        } else {
+            const int row = divide(n, t.group_inverse);
+            ((HOPL_GLOBAL T*)t.dq)[(int64_t)(seq.q0 + row) * t.lddq + (head * t.group + n - row * t.group) * t.cols + c] = (T)(v * t.scale);
         }
     }
 }
@@ -590,15 +615,15 @@ __global__ __launch_bounds__(256) void attention_align_kernel(HopAttentionCopies
 
 template <typename T, int D>
 int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t stream) {
-    constexpr int grid = kCus, kThreads = 256 * kHalves<T, D>, kJoins = kTile / 16;
+    constexpr int grid = kCus, kThreads = 256 * kHalves<T, D>, kJoins = (kCus - 1) * (kTile / 8);
     attention_plan_kernel<<<dim3(2), dim3(kPlanners), 0, stream>>>(t, 32 * kHalves<T, D>, plan.q_tiles, plan.k_tiles);
     if (t.q_rows) {
         attention_dq_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
-        (attention_grad_join_kernel<T, false>)<<<dim3((unsigned)(plan.q_tiles * t.k_heads * kJoins)), dim3(256), 0, stream>>>(t, grid);
+        (attention_grad_join_kernel<T, false>)<<<dim3(kJoins), dim3(256), 0, stream>>>(t, grid);
     }
     if (t.k_rows) {
         attention_dkv_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
-        (attention_grad_join_kernel<T, true>)<<<dim3((unsigned)(plan.k_tiles * t.k_heads * kJoins)), dim3(256), 0, stream>>>(t, grid);
+        (attention_grad_join_kernel<T, true>)<<<dim3(kJoins), dim3(256), 0, stream>>>(t, grid);
     }
     return (int)hipGetLastError();
 }

@@ -1,7 +1,8 @@
 """Attention's kernels, and those of the norm and rotation of queries and keys, against their 64-bit statement (oracle/attention.py), on the GPU.
 
 Tolerances, element by element, come from oracle/attention.py with u = 2^-24 and, where rows are bfloat16, weights rounded by half a step of 2^-8;
-results in bfloat16 are rounded once more: 2^-8 of the result and of the first error's neighbour.
+results in bfloat16 are rounded once more: 2^-8 of the result and of the first error's neighbour.  The gradient may take sum do o from o as it was written, or before
+its rounding: the bounds of what follows from it count the difference of the two, as it is.
 """
 import numpy as np
 import pytest
@@ -50,7 +51,7 @@ def check(dtype, nq, nk, hq, hk, D, causal, scale=None, odd=False, loud=1.0, gra
         t.fill_(float("nan"))
     attention.attention_grad(do, o, lse, q, k, v, dq=outs[0][0], dk=outs[1][0], dv=outs[2][0], **how)
     wants = oa.attention_grad(do64, o64, lse64, q64, k64, v64, *rest)
-    bounds = oa.attention_bounds(do64, o64, lse64, q64, k64, v64, *rest, U, rounding)[2:]
+    bounds = oa.attention_bounds(do64, o64, lse64, q64, k64, v64, *rest, U, rounding, want)[2:]
     for (t, fine), w, b, name in zip(outs, wants, bounds, ("dq", "dk", "dv")):
         close(t, w, b, dtype, name)
         assert fine(), name
