@@ -571,21 +571,31 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTa
     int64_t b0, b1;
     if (!runs_inside(runs, head, seq, &b0, &b1) || b0 != run) return;
     const int all = (KEYS ? seq.nk : seq.nq * t.group) - seq.first, rows = min(kEach, all - first);
-    for (int i = threadIdx.x; i < rows * t.cols * kSums; i += 256) {
-        const int which = KEYS ? i / (rows * t.cols) : 0, j = i - which * rows * t.cols, r = j / t.cols, c = j - r * t.cols, in = first + r, n = seq.first + in;
-        const int64_t place = (int64_t)which * kTile * t.cols + in * t.cols + c;
-        float v = ((const HOPL_GLOBAL float*)part_place(t, b0 - 1, true, kSums))[place];
+    auto columns = [&](auto width) __attribute__((always_inline)) {
+        constexpr int kWidth = decltype(width)::value;
+        typedef float sum __attribute__((ext_vector_type(kWidth)));
+        typedef sum sum_any __attribute__((aligned(4)));
+        const int per_row = t.cols / kWidth;
+        for (int i = threadIdx.x; i < rows * per_row * kSums; i += 256) {
+            const int r = i / (per_row * kSums), j = i - r * per_row * kSums, which = KEYS && j >= per_row, c = (j - which * per_row) * kWidth, in = first + r, n = seq.first + in;
+            const int64_t place = (int64_t)which * kTile * t.cols + in * t.cols + c;
+            sum v = *(const HOPL_GLOBAL sum_any*)(part_place(t, b0 - 1, true, kSums) + place);
 #pragma unroll 4
-        for (int64_t b = b0; b <= b1; ++b) v += ((const HOPL_GLOBAL float*)part_place(t, b, false, kSums))[place];
-        if constexpr (KEYS) {
-            const int64_t row = seq.k0 + n;
-            if (which) ((HOPL_GLOBAL T*)t.dv)[row * t.lddv + head * t.cols + c] = (T)v;
-            else ((HOPL_GLOBAL T*)t.dk)[row * t.lddk + head * t.cols + c] = (T)(v * t.scale);
-        } else {
-            const int row = divide(n, t.group_inverse);
-            ((HOPL_GLOBAL T*)t.dq)[(int64_t)(seq.q0 + row) * t.lddq + (head * t.group + n - row * t.group) * t.cols + c] = (T)(v * t.scale);
+            for (int64_t b = b0; b <= b1; ++b) v += *(const HOPL_GLOBAL sum_any*)(part_place(t, b, false, kSums) + place);
+            T* to;
+            if constexpr (KEYS) {
+                to = (which ? (T*)t.dv + (seq.k0 + n) * t.lddv : (T*)t.dk + (seq.k0 + n) * t.lddk) + head * t.cols + c;
+            } else {
+                const int row = divide(n, t.group_inverse);
+                to = (T*)t.dq + (int64_t)(seq.q0 + row) * t.lddq + (head * t.group + n - row * t.group) * t.cols + c;
+            }
+            const float by = which ? 1.f : t.scale;
+            if constexpr (kWidth == 4) store4(to, 4, v * by);
+            else *(HOPL_GLOBAL T*)to = (T)(v[0] * by);
         }
-    }
+    };
+    if (t.cols % 4 == 0) columns(std::integral_constant<int, 4>());
+    else columns(std::integral_constant<int, 1>());
 }
 
 // ---- rows that the memory unit cannot take, laid out anew -----------------------------------------
