@@ -226,8 +226,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t)
         const int64_t at = part_place(t, p, head, pair);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float x = lane + 64 * i < t.cols ? sums[at * t.cols + lane + 64 * i] : 0.f;
-            if (w != 0.f) v[i] += w * x;
+            const float x = lane + 64 * i < t.cols && w != 0.f ? sums[at * t.cols + lane + 64 * i] : 0.f;
+            v[i] = __builtin_fmaf(w, x, v[i]);
         }
     }
     const float by = total == 0.f ? 0.f : 1.f / total;
@@ -273,14 +273,8 @@ int launch(const HopAttentionTask& t, hipStream_t stream) {
 int hopa_forward_parts(const HopAttentionTask& t, int dtype) {
     (void)dtype;
     const int64_t step = few(t) ? 32 : 128, tiles = (((int64_t)t.q_rows * t.group + step - 1) / step + t.S) * t.k_heads, keys = t.k_rows / t.S;
-#ifndef WANT
-#define WANT 1024
-#define WANT4 512
-#define LST 64
-#define LST4 256
-#endif
-    const int64_t wanted = few(t) ? WANT : WANT4;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((wanted + tiles - 1) / tiles, keys / (few(t) ? LST : LST4)), 64));
+    const int64_t wanted = few(t) ? 1024 : 512, least = few(t) ? 64 : 256;            // workgroups; keys of a part
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((wanted + tiles - 1) / tiles, keys / least), 64));
 }
 
 int hopa_forward(const HopAttentionTask& t, int dtype, void* stream) {
