@@ -102,7 +102,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, p[u][r]);
         if (__any(__builtin_fmaf(most, t.scale_log2, -8.f) > top)) {
-            const float now = fmaxf(top, both_max(most) * t.scale_log2), by = now == -kInf ? 1.f : __builtin_amdgcn_exp2f(top - now);
+            // only of columns with such a score, so that a row's bits do not depend on the rows beside it
+            const float its = both_max(most) * t.scale_log2, now = its - 8.f > top ? its : top, by = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= by;
 #pragma unroll

@@ -657,7 +657,7 @@ HopAttentionPlan hopa_grad_plan(HopAttentionTask* task, int dtype, char* scratch
     p.q_tiles = ((int64_t)t.q_rows * t.group + kTile - 1) / kTile + t.S;
     p.k_tiles = ((int64_t)t.k_rows + kTile - 1) / kTile + t.S;
     auto take = [&](size_t bytes) {
-        char* at = scratch + p.bytes;
+        char* at = (char*)((uintptr_t)scratch + p.bytes);           // scratch is null where only the bytes are asked for
         p.bytes += (bytes + 255) / 256 * 256;
         return at;
     };

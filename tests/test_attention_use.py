@@ -1,0 +1,243 @@
+"""Attention and the rotation as programs use them, on the GPU: columns of one matrix, weights of replicas in a lattice, rows that belong to nobody, hidden values that are
+not finite, streams, graphs, long caches, a whole layer with its gradients."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as oa
+from paper_1902_01064_amd import attention, layers
+from test_attention import check
+from test_layers import DEV, U, begin_of, close, holes, rounded, table
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def made(seed, rows, cols, dtype):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return torch.randn((rows, cols), device=DEV, generator=g).to(DT[dtype])
+
+
+# Many sequences of any lengths, so that tiles are cut between workgroups in every way: each row against the 64-bit statement.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S,longest,hq,hk,D,causal", [(300, 40, 3, 1, 16, True), (70, 200, 2, 2, 64, False), (5, 900, 2, 1, 72, True), (2, 1500, 4, 1, 128, True), (1, 3000, 1, 1, 32, True)])
+def test_many_lengths(dtype, S, longest, hq, hk, D, causal):
+    r = np.random.default_rng(S)
+    n = [int(v) for v in r.integers(0, longest + 1, S)]
+    check(dtype, n, n, hq, hk, D, causal)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 40, 33])
+@pytest.mark.parametrize("nq,nk", [([40, 0, 70], [40, 0, 70]), ([1, 1], [300, 20]), ([100], [30])])
+def test_rows_of_nobody_are_neither_read_nor_written(dtype, D, nq, nk):
+    """NaN in front of the first sequence and behind the last one changes nothing, and results there stay as they are."""
+    hq, hk, before, behind = 4, 2, 3, 5
+    qb, kb = begin_of(nq), begin_of(nk)
+    q, k, v, do = (made(i, n, h * D, dtype) for i, (n, h) in enumerate(((sum(nq), hq), (sum(nk), hk), (sum(nk), hk), (sum(nq), hq))))
+    how = dict(q_heads=hq, k_heads=hk)
+    plain = dict(how, q_begin=table(qb), k_begin=table(kb))
+    o, lse = attention.attention(q, k, v, **plain)
+    grads = attention.attention_grad(do, o, lse, q, k, v, **plain)
+
+    def wide(t, fill):
+        w = torch.full((before + t.shape[0] + behind, t.shape[1]), fill, dtype=t.dtype, device=DEV)
+        w[before:before + t.shape[0]] = t
+        return w
+    shifted = dict(how, q_begin=table(qb + before), k_begin=table(kb + before))
+    nan = float("nan")
+    Q, K, V, DO = (wide(t, nan) for t in (q, k, v, do))
+    O, L = wide(torch.zeros_like(o), 7.0), torch.full((hq, Q.shape[0]), 7.0, device=DEV)
+    attention.attention(Q, K, V, out=O, out_lse=L, **shifted)
+    inside = slice(before, before + sum(nq))
+    assert torch.equal(O[inside], o) and torch.equal(L[:, inside], lse)
+    L2 = L.clone()
+    L[:, inside] = O[inside] = 7.0
+    assert (O == 7.0).all() and (L == 7.0).all()
+    outs = [wide(torch.zeros_like(g), 7.0) for g in grads]
+    attention.attention_grad(DO, wide(o, nan), L2, Q, K, V, dq=outs[0], dk=outs[1], dv=outs[2], **shifted)
+    for g, w in zip(outs, grads):
+        at = slice(before, before + w.shape[0])
+        assert torch.equal(g[at], w)
+        g[at] = 7.0
+        assert (g == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 33])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("n,group", [(50, 1), (200, 3)])
+def test_what_is_hidden_has_no_influence(dtype, D, bad, n, group):
+    """Values that are not finite in the last keys change no earlier query's result; in the first queries, and their gradients, no later key's."""
+    hk, hq = 2, 2 * group
+    q, k, v, do = (made(i, n, h * D, dtype) for i, h in enumerate((hq, hk, hk, hq)))
+    how = dict(q_heads=hq, k_heads=hk)
+    o, lse = attention.attention(q, k, v, **how)
+    dq, dk, dv = attention.attention_grad(do, o, lse, q, k, v, **how)
+    last = n - 3
+    K, V = k.clone(), v.clone()
+    K[last:, 5], V[last:, 1] = bad, bad
+    O, L = attention.attention(q, K, V, **how)
+    assert torch.equal(O[:last], o[:last]) and torch.equal(L[:, :last], lse[:, :last])
+    DQ, _, _ = attention.attention_grad(do, o, lse, q, K, V, **how)
+    assert torch.equal(DQ[:last], dq[:last])
+    Q, DO, early = q.clone(), do.clone(), 4
+    Q[:early, 3], DO[:early, 2] = bad, bad
+    _, DK, DV = attention.attention_grad(DO, o, lse, Q, k, v, **how)
+    assert torch.equal(DK[early:], dk[early:]) and torch.equal(DV[early:], dv[early:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_sequences_results_do_not_depend_on_the_others(dtype):
+    """The other sequences' values: NaN and infinities everywhere in them change nothing."""
+    n, D = [60, 33, 150], 64
+    q, k, v, do = (made(i, sum(n), 2 * D, dtype) for i in range(4))
+    how = dict(q_heads=2, k_heads=2, q_begin=table(begin_of(n)))
+    o, lse = attention.attention(q, k, v, **how)
+    grads = attention.attention_grad(do, o, lse, q, k, v, **how)
+    for t in (q, k, v, do, o):
+        t[60:93] = float("nan")
+    O, _ = attention.attention(q, k, v, **how)
+    others = torch.tensor(list(range(60)) + list(range(93, sum(n))), device=DEV)
+    assert torch.equal(O[others], o[others])
+    for g, w in zip(attention.attention_grad(do, o, lse, q, k, v, **how), grads):
+        assert torch.equal(g[others], w[others])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nq,nk,hq,hk,D", [([300, 20], [300, 20], 4, 2, 128), ([1, 1, 1], [900, 3, 70], 8, 2, 64), ([77], [77], 2, 1, 33)])
+def test_streams_graphs_and_repeats_give_the_same_bits(dtype, nq, nk, hq, hk, D):
+    qb, kb = table(begin_of(nq)), table(begin_of(nk))
+    q, k, v, do = (made(i, n, h * D, dtype) for i, (n, h) in enumerate(((sum(nq), hq), (sum(nk), hk), (sum(nk), hk), (sum(nq), hq))))
+    w = 1 + 0.1 * made(9, 1, D, "f32")
+    pos = torch.arange(sum(nq), dtype=torch.int32, device=DEV)
+
+    def passes():
+        x = attention.rotate(q, hq, 0, q_weight=w, positions=pos, rotary=D // 2 * 2)
+        o, lse = attention.attention(x, k, v, hq, hk, qb, kb)
+        g = attention.attention_grad(do, o, lse, x, k, v, hq, hk, qb, kb)
+        dx, dw, _ = attention.rotate_grad(g[0], q, hq, 0, q_weight=w, positions=pos, rotary=D // 2 * 2)
+        return [o, lse, *g, dx, dw]
+    want = [t.clone() for t in passes()]
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(passes(), want))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        there = passes()
+    here = passes()                                   # both at once
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) and torch.equal(c, b) for a, b, c in zip(there, want, here))
+    graphs = []
+    for _ in range(2):
+        graphs.append((torch.cuda.CUDAGraph(), []))
+        with torch.cuda.graph(graphs[-1][0]):
+            graphs[-1][1].extend(passes())
+    for _ in range(4):
+        for graph, results in graphs:
+            for t in results:
+                t.fill_(float("nan"))
+            graph.replay()
+            passes()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(results, want))
+
+
+def test_a_cache_of_over_four_gigabytes():
+    """Three sequences far apart in it, the last one behind 2^32 bytes; against the same sequences alone."""
+    D, hk, hq, n = 128, 8, 16, [1 << 21, 1 << 18, 300]
+    begin = begin_of(n)
+    k, v = (torch.zeros((int(begin[-1]), hk * D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    assert k.numel() * 2 > 1 << 32
+    k[-300:], v[-300:] = made(1, 300, hk * D, "bf16"), made(2, 300, hk * D, "bf16")
+    q = made(3, 3, hq * D, "bf16")
+    o, lse = attention.attention(q, k, v, hq, hk, table(begin_of([1, 1, 1])), table(begin))
+    alone, alone_lse = attention.attention(q[2:], k[-300:].clone(), v[-300:].clone(), hq, hk)
+    # how keys are cut into parts goes by the call's sizes: weights are rounded for other maxima
+    assert (o[2:].double() - alone.double()).abs().max() <= 2.0 ** -6 * alone.abs().max() and (lse[:, 2:] - alone_lse).abs().max() <= 1e-5
+    assert (o[:2] == 0).all() and torch.allclose(lse[:, 0], torch.full((hq,), float(np.log(n[0])), device=DEV), atol=1e-5)
+
+
+def test_rotation_with_weights_in_a_lattice_and_rows_of_sequences():
+    """Weights read, and their gradients written, where they lie among replicas; positions from the sequences; y in the place of x."""
+    G, D, hq, hk, dtype = 3, 16, 2, 1, "f32"
+    counts, n = [5, 0, 12], [4, 9, 0, 4]
+    x, x64 = rounded(np.random.default_rng(1).standard_normal((17, (hq + hk) * D)), dtype)
+    dy, dy64 = rounded(np.random.default_rng(2).standard_normal(x64.shape), dtype)
+    arena, a64 = rounded(1 + 0.2 * np.random.default_rng(3).standard_normal((7, 40)), "f32")
+    index = [6, 0, 2]
+    begin, pos = begin_of(counts), np.concatenate([np.arange(v) for v in n])
+    how = dict(q_heads=hq, k_heads=hk, q_weight=arena[:, :D], k_weight=arena[:, 20:20 + D], row_begin=table(begin), index=index, seq_begin=table(begin_of(n)), base=100.0)
+    rest = (hq, hk, a64[index, :D], a64[index, 20:20 + D], begin, pos, D, False, 100.0, "rms", float(np.float32(1e-5)))
+    bounds = oa.rotate_bounds(dy64, x64, *rest, U)
+    y = x.clone()
+    assert attention.rotate(y, out=y, **how) is y
+    close(y, oa.rotate(x64, *rest), bounds[0], dtype, "y")
+    grads, unharmed = holes(9, 40, "f32", 0, 0)
+    grads.fill_(7.0)
+    g = dy.clone()
+    attention.rotate_grad(g, x, dx=g, dq_weight=grads[:, :D], dk_weight=grads[:, 20:20 + D], grad_index=[8, 1, 5], **how)
+    wants = oa.rotate_grad(dy64, x64, *rest)
+    close(g, wants[0], bounds[1], dtype, "dx")
+    close(grads[[8, 1, 5], :D], wants[1], bounds[2], "f32", "dq_weight")
+    close(grads[[8, 1, 5], 20:20 + D], wants[2], bounds[3], "f32", "dk_weight")
+    assert (grads[[0, 2, 3, 4, 6, 7]] == 7.0).all() and (grads[:, D:20] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,limit", [("f32", 2e-4), ("bf16", 0.06)])
+def test_a_layer_of_workers_and_its_gradients(dtype, limit):
+    """Products with every worker's own weights, the norm and rotation of queries and keys where they lie, attention over the workers' sequences, the product behind it;
+    all in columns of one matrix, gradients too.  Against the chain of 64-bit statements.
+
+    fp32: five stages, each a sum of up to 48 products, (48 + 26) 2^-24 of what meets, which cancels to an eighth at worst on the norm over a matrix: 5 * 4.4e-6 * 8 = 1.8e-4.
+    bfloat16: every stage's result is rounded by up to 2^-8, ten of them from x to a gradient of x, errors of one do not cancel another's: 10 * 2^-8 = 0.04, half as much again for
+    the weights of the softmax and their gradients."""
+    G, counts, n = 2, [40, 57], [13, 27, 57]
+    hq, hk, D, width = 4, 2, 12, 24
+    rows, wide = sum(counts), (hq + 2 * hk) * D
+    r = np.random.default_rng(8)
+    x, x64 = rounded(r.standard_normal((rows, width)), dtype)
+    wi, wi64 = rounded(r.standard_normal((G, wide, width)) * width ** -0.5, dtype)
+    wo, wo64 = rounded(r.standard_normal((G, width, hq * D)) * (hq * D) ** -0.5, dtype)
+    nq, nq64 = rounded(1 + 0.2 * r.standard_normal((G, D)), "f32")
+    nk, nk64 = rounded(1 + 0.2 * r.standard_normal((G, D)), "f32")
+    dout, dout64 = rounded(r.standard_normal((rows, width)), dtype)
+    begin, seq = begin_of(counts), begin_of(n)
+    pos = np.concatenate([np.arange(v) for v in n])
+    rb, sb = table(begin), table(seq)
+    turn = dict(q_heads=hq, k_heads=hk, q_weight=nq, k_weight=nk, row_begin=rb, seq_begin=sb)
+    heads, both = dict(q_heads=hq, k_heads=hk, q_begin=sb), (hq + hk) * D
+    # forwards
+    qkv = layers.product(x, wi, rb)
+    raw = qkv[:, :both].clone()
+    attention.rotate(qkv[:, :both], out=qkv[:, :both], **turn)
+    q, k, v = qkv[:, :hq * D], qkv[:, hq * D:both], qkv[:, both:]
+    o, lse = attention.attention(q, k, v, **heads)
+    out = layers.product(o, wo, rb)
+    # backwards
+    do = layers.product(dout, wo, rb, transposed=True)
+    d = torch.empty_like(qkv)
+    attention.attention_grad(do, o, lse, q, k, v, dq=d[:, :hq * D], dk=d[:, hq * D:both], dv=d[:, both:], **heads)
+    _, dnq, dnk = attention.rotate_grad(d[:, :both], raw, dx=d[:, :both], **turn)
+    dwi = layers.product_grad(d, x, rb)
+    dx = layers.product(d, wi, rb, transposed=True)
+    dwo = layers.product_grad(dout, o, rb)
+    # in 64 bits
+    by = [slice(int(begin[g]), int(begin[g + 1])) for g in range(G)]
+    each = lambda a, w: np.concatenate([a[s] @ w[g].T for g, s in enumerate(by)])          # noqa: E731
+    grad = lambda a, b: np.stack([a[s].T @ b[s] for s in by])                              # noqa: E731
+    t = each(x64, wi64)
+    rest = (hq, hk, nq64, nk64, begin, pos, D, False, 10000.0, "rms", float(np.float32(1e-5)))
+    qk = oa.rotate(t[:, :both], *rest)
+    args = (qk[:, :hq * D], qk[:, hq * D:], t[:, both:])
+    how = (hq, hk, seq, seq, True, D ** -0.5)
+    o64, lse64 = oa.attention(*args, *how)
+    do64 = each(dout64, wo64.transpose(0, 2, 1))
+    g64 = oa.attention_grad(do64, o64, lse64, *args, *how)
+    dt, dnq64, dnk64 = oa.rotate_grad(np.concatenate(g64[:2], 1), t[:, :both], *rest)
+    d64 = np.concatenate([dt, g64[2]], 1)
+    for name, got, want in (("out", out, each(o64, wo64)), ("dx", dx, each(d64, wi64.transpose(0, 2, 1))), ("dwi", dwi, grad(d64, x64)), ("dwo", dwo, grad(dout64, o64)),
+                            ("dnq", dnq, dnq64), ("dnk", dnk, dnk64)):
+        error = np.linalg.norm(got.double().cpu().numpy() - want) / np.linalg.norm(want)
+        assert error <= limit, (name, error)
