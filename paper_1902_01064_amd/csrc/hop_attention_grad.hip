@@ -113,8 +113,11 @@ __device__ __forceinline__ int64_t run_of_block(int64_t blocks) {
     return blocks == n && n % 8 == 0 ? (int64_t)(at % 8) * (n / 8) + at / 8 : at;
 }
 // A part's place: rows of `cols` floats.  A tile's first part is the last thing that its workgroup does, any other one the first, so there are two at most.
-__device__ __forceinline__ float* part_place(const HopAttentionTask& t, int64_t block, bool first_part, int sums) {
-    return t.partial + (block * 2 + (first_part ? 1 : 0)) * sums * kTile * t.cols;
+// Those of dq, one matrix each, lie in front of those of dk and dv, two each.
+template <bool KEYS>
+__device__ __forceinline__ float* part_place(const HopAttentionTask& t, int64_t block, bool first_part) {
+    const int64_t matrix = kTile * t.cols, number = block * 2 + (first_part ? 1 : 0);
+    return t.partial + (KEYS ? kCus * 2 + number * 2 : number) * matrix;
 }
 
 // The second half's sums, added to the first one's.  Nobody uses the pool any more.
@@ -335,7 +338,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         add_halves<kU, kH>(pool, half, wave, dq);
         if (!live || half) continue;
         if (first_stage > 0 || last_stage < seq.stages)
-            store_columns<float, D>(part_place(t, block, first_stage == 0, 1) + (int64_t)(pair - first) * t.cols, t.cols, dq, 1.f);
+            store_columns<float, D>(part_place<false>(t, block, first_stage == 0) + (int64_t)(pair - first) * t.cols, t.cols, dq, 1.f);
         else
             store_columns<T, D>((T*)t.dq + at * t.lddq + column, t.cols, dq, t.scale);
     }
@@ -545,7 +548,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             const int column = cut * kSumCols, cols = t.cols - column;
             if (!live || half || cols <= 0) continue;
             if (first_stage > 0 || last_stage < seq.stages) {
-                float* part = part_place(t, block, first_stage == 0, 2) + (int64_t)(key - first) * t.cols;
+                float* part = part_place<true>(t, block, first_stage == 0) + (int64_t)(key - first) * t.cols;
                 store_columns<float, kSumCols>(part + column, cols, dk, 1.f);
                 store_columns<float, kSumCols>(part + kTile * t.cols + column, cols, dv, 1.f);
             } else {
@@ -559,7 +562,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
 // ---- parts, joined in their order -------------------------------------------------------------
 // 8 rows of the tile in which run number blockIdx.x / 16 + 1 begins, if it is the first one to do so.  A part is `sums` matrices: dq, or dk and dv.
 template <typename T, bool KEYS>
-__global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTask t, int most) {
+__device__ __forceinline__ void join_tile(const HopAttentionTask& t, int most) {
     constexpr int kSums = KEYS ? 2 : 1, kEach = 8;
     const Runs runs(KEYS ? t.k_plan : t.q_plan, t.k_heads, most);
     const int64_t run = blockIdx.x / (kTile / kEach) + 1, tiles = runs.plan->tiles;
@@ -579,9 +582,9 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTa
         for (int i = threadIdx.x; i < rows * per_row * kSums; i += 256) {
             const int r = i / (per_row * kSums), j = i - r * per_row * kSums, which = KEYS && j >= per_row, c = (j - which * per_row) * kWidth, in = first + r, n = seq.first + in;
             const int64_t place = (int64_t)which * kTile * t.cols + in * t.cols + c;
-            sum v = *(const HOPL_GLOBAL sum_any*)(part_place(t, b0 - 1, true, kSums) + place);
+            sum v = *(const HOPL_GLOBAL sum_any*)(part_place<KEYS>(t, b0 - 1, true) + place);
 #pragma unroll 4
-            for (int64_t b = b0; b <= b1; ++b) v += *(const HOPL_GLOBAL sum_any*)(part_place(t, b, false, kSums) + place);
+            for (int64_t b = b0; b <= b1; ++b) v += *(const HOPL_GLOBAL sum_any*)(part_place<KEYS>(t, b, false) + place);
             T* to;
             if constexpr (KEYS) {
                 to = (which ? (T*)t.dv + (seq.k0 + n) * t.lddv : (T*)t.dk + (seq.k0 + n) * t.lddk) + head * t.cols + c;
@@ -596,6 +599,11 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTa
     };
     if (t.cols % 4 == 0) columns(std::integral_constant<int, 4>());
     else columns(std::integral_constant<int, 1>());
+}
+template <typename T>
+__global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTask t, int most) {
+    if (blockIdx.y) join_tile<T, true>(t, most);
+    else join_tile<T, false>(t, most);
 }
 
 // ---- rows that the memory unit cannot take, laid out anew -----------------------------------------
@@ -627,14 +635,9 @@ template <typename T, int D>
 int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t stream) {
     constexpr int grid = kCus, kThreads = 256 * kHalves<T, D>, kJoins = (kCus - 1) * (kTile / 8);
     attention_plan_kernel<<<dim3(2), dim3(kPlanners), 0, stream>>>(t, 32 * kHalves<T, D>, plan.q_tiles, plan.k_tiles);
-    if (t.q_rows) {
-        attention_dq_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
-        (attention_grad_join_kernel<T, false>)<<<dim3(kJoins), dim3(256), 0, stream>>>(t, grid);
-    }
-    if (t.k_rows) {
-        attention_dkv_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
-        (attention_grad_join_kernel<T, true>)<<<dim3(kJoins), dim3(256), 0, stream>>>(t, grid);
-    }
+    if (t.q_rows) attention_dq_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
+    if (t.k_rows) attention_dkv_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
+    attention_grad_join_kernel<T><<<dim3(kJoins, 2), dim3(256), 0, stream>>>(t, grid);
     return (int)hipGetLastError();
 }
 
@@ -665,7 +668,7 @@ HopAttentionPlan hopa_grad_plan(HopAttentionTask* task, int dtype, char* scratch
     t.terms = (float*)take((size_t)2 * t.k_heads * t.group * t.q_rows * 4);
     t.q_plan = take(plan_bytes(p.q_tiles));
     t.k_plan = take(plan_bytes(p.k_tiles));
-    t.partial = (float*)take((size_t)kCus * 2 * 2 * kTile * t.cols * 4);          // two parts of a workgroup, each of dk and dv
+    t.partial = (float*)take((size_t)kCus * 2 * 3 * kTile * t.cols * 4);          // two parts of a workgroup, of dq, dk and dv
     // copies of what the memory unit cannot take
     const int elem = dtype == HOP_BF16 ? 2 : 4, chunk = 16 / elem, head = (t.cols + chunk - 1) / chunk * chunk;
     auto fits = [&](const void* m, int64_t ld) { return ((uintptr_t)m & 15u) == 0 && (ld * elem) % 16 == 0; };
