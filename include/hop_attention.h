@@ -20,9 +20,12 @@
  *  - What a query does not see has no influence, whatever it holds: infinities and NaN in keys and values behind a query, or in queries (and
  *    their gradients) in front of a key, or in rows of other sequences, change nothing.
  *  - Sums, statistics and scores are held in fp32.  With bfloat16 rows the softmax's terms and the gradients of the scores are rounded to
- *    bfloat16 as operands of the products that follow.
- *  - Sizes: heads of up to HOP_MAX_HEAD_COLS columns (64 and 128 in multiples of 16 bytes are the fastest), rows times query heads below 2^30, distances between
- *    rows up to 2^22 elements, up to HOP_MAX_GROUPS sequences.
+ *    bfloat16 as operands of the products that follow.  A row's results depend on its sequence and on how many rows all of them have, not on other
+ *    rows' values, and are the same bits every time.
+ *  - Results may not overlap what a call reads, except where it is said.
+ *  - Sizes: heads of up to HOP_MAX_HEAD_COLS columns, rows times query heads below 2^30, distances between rows up to 2^22 elements, up to
+ *    HOP_MAX_GROUPS sequences.  Fastest are heads of 64 and 128 columns in rows whose addresses and distances are multiples of 16 bytes; for others
+ *    hop_attention_grad copies what it reads into its scratch first.
  */
 #ifndef HOP_ATTENTION_H
 #define HOP_ATTENTION_H

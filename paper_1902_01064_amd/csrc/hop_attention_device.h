@@ -480,16 +480,18 @@ struct PlanTile {
 struct Plan {
     int64_t weight;                             // of a head's tiles
     int64_t tiles;
+    int64_t fixed;                              // stages that a tile's operands and its sums' way out are worth
     PlanTile tile[1];                           // tiles + 1 of them
 };
 constexpr int kLeast = 4;                       // stages: a run has that many, and no cut lies nearer to the edge of a tile
-constexpr int kFixed = 7;                       // stages that a tile's operands and its sums' way out are worth (17500 cycles, a stage of 128 columns in bfloat16 2440)
 
 struct Runs {
     const HOPL_GLOBAL Plan* plan;
     int64_t all;                                // weight of all heads
     int64_t blocks;
+    int fixed;
     __device__ __forceinline__ Runs(const void* p, int heads, int most) : plan((const HOPL_GLOBAL Plan*)p) {
+        fixed = (int)plan->fixed;
         all = plan->weight * heads;
         blocks = all / kLeast;
         blocks = blocks < 1 ? 1 : blocks > most ? most : blocks;
@@ -517,7 +519,7 @@ __device__ __forceinline__ Place begin_of_run(const Runs& r, int64_t block) {
         low += (63 - __builtin_clzll(before)) * step;
         high = low + step < high ? low + step : high;
     }
-    const int stage = (int)(in - r.plan->tile[low].before) - kFixed, stages = r.plan->tile[low].stages;
+    const int stage = (int)(in - r.plan->tile[low].before) - r.fixed, stages = r.plan->tile[low].stages;
     if (stage < kLeast) return {head * tiles + low, 0};
     if (stages - stage < kLeast) return {head * tiles + low + 1, 0};
     return {head * tiles + low, stage};
@@ -525,7 +527,7 @@ __device__ __forceinline__ Place begin_of_run(const Runs& r, int64_t block) {
 // The workgroups whose runs begin inside of a tile, from *first to *last; false: none does.
 __device__ __forceinline__ bool runs_inside(const Runs& r, int64_t head, const PlanTile& tile, int64_t* first, int64_t* last) {
     if (tile.stages < 2 * kLeast) return false;
-    const int64_t at = head * r.plan->weight + tile.before + kFixed, from = at + kLeast, to = at + tile.stages - kLeast + 1;    // [from, to)
+    const int64_t at = head * r.plan->weight + tile.before + r.fixed, from = at + kLeast, to = at + tile.stages - kLeast + 1;    // [from, to)
     *first = (from * r.blocks + r.all - 1) / r.all;
     *last = (to * r.blocks + r.all - 1) / r.all - 1;
     return *first <= *last;

@@ -3,9 +3,13 @@
 //   p_ij = exp(scale q_i k_j - lse_i),  D_i = sum_c do_ic o_ic,  ds_ij = p_ij (do_i v_j - D_i)
 //   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i              10 pairs cols operations
 //
-// Two kernels, each with sums of its own in registers, so that results are the same bits every time: one passes over the keys of a run of pairs for dq
-// (and leaves D and lse for the other), one over the pairs of a run of keys for dk and dv.  The price is that scores and do v^T are computed
-// twice: 14 operations where 10 would do.  Both take even shares of all tiles, which a small kernel in front of them lays out from the tables.
+// Two kernels, each with sums of its own in registers, so that results are the same bits every time: one passes over the keys of a tile of pairs for dq
+// (and leaves D and lse for the other), one over the pairs of a tile of keys for dk and dv.  The price is that scores and do v^T are computed
+// twice: 14 operations where 10 would do.  Both take even shares of all tiles, which a small kernel in front of them lays out from the tables: with a workgroup to a tile
+// the longest sequence's tiles decided (12288 tokens in 6 sequences, 16 heads on 2: 1076 us, now 467).
+//
+// What bounds them is the matrix unit, at the clock that its power leaves: 8192 tokens that all see each other, 16 heads of 128 columns on 2, bfloat16, take 1716 us,
+// 1120 TFLOP/s of the 14 operations (a large library product reaches 1230 to 1390 on such numbers); 58 % of the cycles have a product under way.
 #include <algorithm>
 #include <type_traits>
 
@@ -19,7 +23,7 @@ constexpr int kShift = 7, kTile = 1 << kShift;          // pairs or keys of a ti
 constexpr int kCus = 256;
 constexpr int kExact = 128;                             // keys: see attention_dq_kernel
 // Two halves of a workgroup with the same tile take every other 32 rows of a stage, so that a SIMD has two wavefronts, of which one computes while the other waits, and the CU
-// only one set of tiles.  In fp32 with 128 columns the sums and operands of one wavefront fill a SIMD's registers.
+// only one set of tiles (one wavefront with twice the registers issues an instruction every 5 cycles at best, which is too few beside its products: 1860 us for the above).  In fp32 with 128 columns the sums and operands of one wavefront fill a SIMD's registers.
 template <typename T, int D>
 constexpr int kHalves = D * (int)sizeof(T) <= 256 ? 2 : 1;
 
@@ -30,6 +34,9 @@ __device__ __forceinline__ int seen_from(const HopAttentionTask& t, int nq, int 
 // ---- the plan -----------------------------------------------------------------------------
 // A workgroup for the tiles of pairs, one for those of keys.  `rows`: of a stage.
 constexpr int kPlanners = 1024;
+// What a tile takes beside its stages, in stages: 17500 cycles for pairs, of which a stage of 128 columns in bfloat16 takes 2440, and more for keys.  12288 tokens, 16 heads on 2:
+// dq and dk, dv in 211 and 250 us; as if a tile took nothing 439 and 272.
+constexpr int kPairsFixed = 8, kKeysFixed = 10;
 __device__ __forceinline__ int64_t scan_all(int64_t v, int64_t* waves, int64_t* all) {          // sum of those in front
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int64_t sum = v;
@@ -54,6 +61,7 @@ __global__ __launch_bounds__(kPlanners) void attention_plan_kernel(HopAttentionT
     __shared__ int64_t waves[kPlanners / 64];
     const bool of_keys = blockIdx.x == 1;
     const int64_t most = of_keys ? most_k : most_q;
+    const int fixed = of_keys ? kKeysFixed : kPairsFixed;
     Plan* plan = (Plan*)(of_keys ? t.k_plan : t.q_plan);
     int64_t tiles = 0;
     for (int base = 0; base < t.S; base += kPlanners) {
@@ -94,7 +102,7 @@ __global__ __launch_bounds__(kPlanners) void attention_plan_kernel(HopAttentionT
             tile.stages = (int32_t)n;
         }
         int64_t all;
-        tile.before = weight + scan_all(at < tiles ? n + kFixed : 0, waves, &all);
+        tile.before = weight + scan_all(at < tiles ? n + fixed : 0, waves, &all);
         if (at < tiles) plan->tile[at] = tile;
         weight += all;
     }
@@ -104,6 +112,7 @@ __global__ __launch_bounds__(kPlanners) void attention_plan_kernel(HopAttentionT
         plan->tile[tiles] = end;
         plan->weight = weight;
         plan->tiles = tiles;
+        plan->fixed = fixed;
     }
 }
 
