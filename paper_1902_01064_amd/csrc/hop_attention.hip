@@ -8,7 +8,7 @@
 //
 // With many queries the matrix unit bounds it, and the exponentials beside it: 8192 tokens that all see each other, 16 heads of 128 columns on 2, bfloat16, take 525 us, 1047
 // TFLOP/s; 53 % of the cycles have a product under way (writing down an order of products and exponentials within a wavefront changed nothing: two wavefronts to a SIMD fill each
-// other's gaps).  With few, the keys' and values' bytes: 16 sequences of 16384 tokens in 215 us, 5.0 TB/s, of which joining the parts takes 7.
+// other's gaps).  With few, the keys' and values' bytes: 16 sequences of 16384 tokens in 206 us, 5.2 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -27,19 +27,45 @@ __device__ __forceinline__ int64_t part_place(const HopAttentionTask& t, int par
     return ((int64_t)part * t.k_heads + head) * ((int64_t)t.q_rows * t.group) + pair;
 }
 
-template <typename T, int D, bool FED, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 : 2) void attention_kernel(HopAttentionTask t) {
+// FEW: the wavefronts of a workgroup have the same 32 pairs and every so many stages of the keys each, buffers of their own, and no barrier before they add up what they have.
+// One wavefront alone fetches keys no faster, and as parts of a launch they would need another one to be joined: 4 sequences of 500
+// keys 14.3 us a call, now 10.3; 131072 keys of one 79, now 44.
+template <typename T, int D>
+constexpr int kFewRows = D * (int)sizeof(T) >= 256 ? 32 : 64;
+template <typename T, int D>
+constexpr int kFewWaves = 32768 / (kFewRows<T, D> * D * (int)sizeof(T));
+
+template <typename T, int D, bool FED, bool FEW>
+__global__ __launch_bounds__((FEW ? kFewWaves<T, D> : 4) * 64, (FEW || (sizeof(T) == 4 && D > 64) ? 1 : 2)) void attention_kernel(HopAttentionTask t) {
     typedef Tile<T, D> L;
-    constexpr int NT = NW * 64, kRows = kTileRows<T, D>, kBytes = kRows * L::kLine, kU = D / 32;
-    constexpr int kShift = NW == 4 ? 7 : 5, kAtOnce = sizeof(T) == 4 ? kRows / 32 : 1;
+    constexpr int kWaves = FEW ? kFewWaves<T, D> : 4, NT = FEW ? 64 : kWaves * 64;           // threads that fill a tile
+    constexpr int kRows = FEW ? kFewRows<T, D> : kTileRows<T, D>, kBytes = kRows * L::kLine, kU = D / 32, kStep = (FEW ? kWaves : 1) * kRows;
+    constexpr int kShift = FEW ? 5 : 7, kAtOnce = sizeof(T) == 4 ? kRows / 32 : 1;
     // arrays of their own, so that the compiler knows that reads of one stage need not wait for loads into the other
-    __shared__ __attribute__((aligned(16))) char sk0[kBytes], sv0[kBytes], sk1[kBytes], sv1[kBytes];
+    constexpr int kAll = (FEW ? kWaves : 1) * kBytes;
+    __shared__ __attribute__((aligned(16))) char all_k0[kAll], all_v0[kAll], all_k1[kAll], all_v1[kAll];
     const int head = blockIdx.x % t.k_heads, rest = blockIdx.x / t.k_heads, part = rest % t.parts;
     int s, first;
     if (!find_tile<true>(t.q_begin, t.S, t.q_rows, t.group, kShift, rest / t.parts, &s, &first)) return;
     const Sequence seq = sequence(t, s);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hi = lane >> 5;
-    const int pairs = seq.nq * t.group, mine = first + wave * 32;            // the wavefront's first pair
+    const int pairs = seq.nq * t.group, mine = first + (FEW ? 0 : wave * 32);            // the wavefront's first pair
+    const int own = FEW ? wave * kBytes : 0;
+    char *const sk0 = all_k0 + own, *const sv0 = all_v0 + own, *const sk1 = all_k1 + own, *const sv1 = all_v1 + own;
+    // with everyone who shares a buffer
+    auto meet = [&]() __attribute__((always_inline)) {
+        if constexpr (FEW) asm volatile("" ::: "memory");
+        else __syncthreads();
+    };
+    auto arrive_here = [&]() __attribute__((always_inline)) {
+        if constexpr (FEW) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0x0070);         // vmcnt(0) lgkmcnt(0)
+            asm volatile("" ::: "memory");
+        } else {
+            arrive();
+        }
+    };
     const int pair = mine + (lane & 31);
     const bool live = pair < pairs;
     const int row = live ? divide(pair, t.group_inverse) : 0, its = live ? pair - row * t.group : 0;
@@ -54,8 +80,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 
     const int all_see_here = visible_of(first);                                       // of the workgroup's
     const int chunk = (seq.nk + t.parts - 1) / t.parts, whole = (chunk + kRows - 1) / kRows * kRows;
     const int64_t from = (int64_t)part * whole;
-    const int begin = from < seq.nk ? (int)from : seq.nk;
-    const int end = min(min(begin + whole, seq.nk), visible_of(min(first + (1 << kShift), pairs) - 1));
+    const int part_begin = from < seq.nk ? (int)from : seq.nk, begin = part_begin + (FEW ? wave * kRows : 0);
+    const int end = min(min(part_begin + whole, seq.nk), visible_of(min(first + (1 << kShift), pairs) - 1));
 
     const Rows gk = {t.ldk, 1, 0, t.cols}, gv = {t.ldv, 1, 0, t.cols};
     Feed<T, D, kRows, NT, FED, false> feed_k, feed_v;
@@ -146,35 +172,75 @@ __global__ __launch_bounds__(NW * 64, NW == 1 || (sizeof(T) == 4 && D > 64) ? 1 
         issue(sk0, sv0, begin);
         put(sk0, sv0);
     }
-    for (int key = begin; key < end; key += 2 * kRows) {
-        arrive();
-        const bool second = key + kRows < end, third = key + 2 * kRows < end;
-        if (second) issue(sk1, sv1, key + kRows);
+    for (int key = begin; key < end; key += 2 * kStep) {
+        arrive_here();
+        const bool second = key + kStep < end, third = key + 2 * kStep < end;
+        if (second) issue(sk1, sv1, key + kStep);
         turn(sk0, sv0, key);
         if (!second) break;
         put(sk1, sv1);
-        arrive();
-        if (third) issue(sk0, sv0, key + 2 * kRows);
-        turn(sk1, sv1, key + kRows);
+        arrive_here();
+        if (third) issue(sk0, sv0, key + 2 * kStep);
+        turn(sk1, sv1, key + kStep);
         if (third) put(sk0, sv0);
     }
     if (t.causal) {
-        if (__syncthreads_or(live && !all_finite(o))) {
+        const bool odd = live && !all_finite(o);
+        if (FEW ? __any(odd) : __syncthreads_or(odd)) {
             clear();
-            for (int key = begin; key < end; key += kRows) {
+            for (int key = begin; key < end; key += kStep) {
                 issue(sk0, sv0, key);
                 put(sk0, sv0);
-                arrive();
-                if (key + kRows > all_see_here) {
+                arrive_here();
+                if (key + kRows > (FEW ? all_see : all_see_here)) {
                     add_not_finite<T, D, D>(sv0, 0, 0, min(kRows, seq.nk - key), o, [&](int j) { return key + j < limit; });
-                    __syncthreads();
+                    meet();
                     drop_not_finite<T, kBytes, NT>(sv0);
-                    __syncthreads();
+                    arrive_here();
                 }
                 turn(sk0, sv0, key);
-                __syncthreads();
+                arrive_here();
             }
         }
+    }
+    if constexpr (FEW) {
+        // The wavefronts' sums at the largest of their maxima, added in their order by the first one.
+        __shared__ float tops[kWaves][64], sums[kWaves][64];
+        tops[wave][lane] = top;
+        __syncthreads();
+        float most = -kInf;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, tops[w][lane]);
+        const float by = top == -kInf ? 0.f : __builtin_amdgcn_exp2f(top - most);
+        sums[wave][lane] = top == -kInf ? sum : sum * by;              // where it is not zero, NaN
+        auto place = [&](int w, int c) __attribute__((always_inline)) {           // of unit c: the wavefront's own buffers, of which it needs no more than these two
+            return (c * 4096 < kBytes ? all_k0 + w * kBytes + c * 4096 : all_v0 + w * kBytes + c * 4096 - kBytes) + lane * 16;
+        };
+        if (wave)
+#pragma unroll
+            for (int c = 0; c < kU; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *(f32x4*)(place(wave, c) + e * 1024) = {o[c][4 * e] * by, o[c][4 * e + 1] * by, o[c][4 * e + 2] * by, o[c][4 * e + 3] * by};
+        __syncthreads();
+        if (wave) return;
+        top = most;
+        sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += sums[w][lane];
+#pragma unroll
+        for (int c = 0; c < kU; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[c][e] *= by;
+        for (int w = 1; w < kWaves; ++w)
+#pragma unroll
+            for (int c = 0; c < kU; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 more = *(const f32x4*)(place(w, c) + e * 1024);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[c][4 * e + i] += more[i];
+                }
     }
 
     const float total = both_sum(sum), base = top == -kInf ? 0.f : top;
@@ -244,7 +310,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t)
     if (t.lse && lane == 0) ((HOPL_GLOBAL float*)t.lse)[(int64_t)h * t.q_rows + row] = total == 0.f ? -kInf : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-// Few pairs to a sequence: a wavefront takes them all, and parts are short (500 keys of 4 sequences: parts of 64 keys, 8 us; of 256, 12).
+// Few pairs to a sequence.
 bool few(const HopAttentionTask& t) { return (int64_t)t.q_rows * t.group <= (int64_t)32 * t.S; }
 
 template <typename T, int D, bool FED>
@@ -252,10 +318,10 @@ int launch(const HopAttentionTask& t, hipStream_t stream) {
     const int64_t pairs = (int64_t)t.q_rows * t.group;
     if (few(t)) {
         const int64_t grid = ((pairs + 31) / 32 + t.S) * t.k_heads * t.parts;
-        attention_kernel<T, D, FED, 1><<<dim3((unsigned)grid), dim3(64), 0, stream>>>(t);
+        attention_kernel<T, D, FED, true><<<dim3((unsigned)grid), dim3(kFewWaves<T, D> * 64), 0, stream>>>(t);
     } else {
         const int64_t grid = ((pairs + 127) / 128 + t.S) * t.k_heads * t.parts;
-        attention_kernel<T, D, FED, 4><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(t);
+        attention_kernel<T, D, FED, false><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(t);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && t.parts > 1) {
@@ -278,7 +344,9 @@ int launch(const HopAttentionTask& t, hipStream_t stream) {
 int hopa_forward_parts(const HopAttentionTask& t, int dtype) {
     (void)dtype;
     const int64_t step = few(t) ? 32 : 128, tiles = (((int64_t)t.q_rows * t.group + step - 1) / step + t.S) * t.k_heads, keys = t.k_rows / t.S;
-    const int64_t wanted = few(t) ? 1024 : 512, least = few(t) ? 64 : 256;            // workgroups; keys of a part
+    // Workgroups, and keys of a part: with few pairs a workgroup to a CU (the next token of 32 sequences of 2048 tokens, 32 heads on 8 of 128: 46.5 us, with two 54), and no parts where
+    // its wavefronts have little to do (4000 keys in parts of 512 16 us, of 1024 20).
+    const int64_t wanted = few(t) ? 256 : 512, least = few(t) ? 512 : 256;
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((wanted + tiles - 1) / tiles, keys / least), 64));
 }
 

@@ -191,9 +191,11 @@ struct Feed {
     typename L::frag held[FED ? 1 : kLoads];
     int rest;
 
-    static __device__ __forceinline__ int line(int i) { return (i * NT + (int)threadIdx.x) / L::kPlaces; }
+    // NT of 64: a wavefront fills a tile of its own
+    static __device__ __forceinline__ int thread() { return NT == 64 ? threadIdx.x & 63 : threadIdx.x; }
+    static __device__ __forceinline__ int line(int i) { return (i * NT + thread()) / L::kPlaces; }
     static __device__ __forceinline__ int chunk(int i) {
-        const int j = i * NT + threadIdx.x;
+        const int j = i * NT + thread();
         return FED ? (j % L::kPlaces) ^ L::swizzle(j / L::kPlaces) : j % L::kPlaces;
     }
     // rest_: how many heads of the first row belong to pairs in front of the tile
@@ -215,7 +217,7 @@ struct Feed {
         if constexpr (FED) {
             const int64_t end = PAIRS ? divide(rest + count - 1, g.inverse) * g.ld + g.group * g.cols : (count - 1) * g.ld + g.cols;
             const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(end * sizeof(T)), 0x00020000);
-            const int wave = threadIdx.x >> 6;
+            const int wave = thread() >> 6;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(stage + (i * NT + wave * 64) * 16), 16, place[i], 0, 0, 0);
@@ -346,7 +348,7 @@ __device__ __forceinline__ void add_not_finite(const char* s, int column, int fr
 }
 template <typename T, int BYTES, int NT>
 __device__ __forceinline__ void drop_not_finite(char* s) {
-    for (int i = threadIdx.x; i < BYTES / (int)sizeof(T); i += NT)
+    for (int i = NT == 64 ? threadIdx.x & 63 : threadIdx.x; i < BYTES / (int)sizeof(T); i += NT)
         if (!(__builtin_fabsf((float)((T*)s)[i]) < kInf)) ((T*)s)[i] = (T)0.f;
 }
 

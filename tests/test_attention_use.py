@@ -89,6 +89,24 @@ def test_what_is_hidden_has_no_influence(dtype, D, bad, n, group):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 33])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_is_hidden_from_the_first_of_a_few_tokens(dtype, D, bad):
+    """The last two of three new tokens of each sequence hold values that are not finite; the first one does not see them."""
+    n, hq, hk = [1500, 90, 3], 4, 2
+    begin, q_begin = begin_of(n), begin_of([3, 3, 3])
+    q, k, v = made(1, 9, hq * D, dtype), made(2, sum(n), hk * D, dtype), made(3, sum(n), hk * D, dtype)
+    how = dict(q_heads=hq, k_heads=hk, q_begin=table(q_begin), k_begin=table(begin))
+    o, lse = attention.attention(q, k, v, **how)
+    for e in begin[1:]:
+        k[e - 2:e, 3], v[e - 1, 7] = bad, bad
+    O, L = attention.attention(q, k, v, **how)
+    first = torch.tensor(q_begin[:-1], device=DEV).long()
+    assert torch.equal(O[first], o[first]) and torch.equal(L[:, first], lse[:, first])
+    assert torch.isfinite(O[first]).all() and not torch.isfinite(O[first + 2]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_sequences_results_do_not_depend_on_the_others(dtype):
     """The other sequences' values: NaN and infinities everywhere in them change nothing."""
     n, D = [60, 33, 150], 64
