@@ -85,10 +85,6 @@ HopAttentionTask attention_task(const hop_attention_args* a) {
     t.ldq = a->ldq; t.ldk = a->ldk; t.ldv = a->ldv;
     return t;
 }
-size_t forward_bytes(const hop_attention_args* a, int parts) {
-    return parts > 1 ? (size_t)parts * a->q_rows * a->q_heads * (a->cols + 2) * 4 : 0;
-}
-
 bool attention_grads_ok(const hop_attention_args* a, const hop_attention_grads* g) {
     if (!attention_ok(a) || !g) return false;
     const size_t e = type_bytes(a->dtype);
@@ -154,7 +150,8 @@ int hop_rotate_grad(const hop_rotate_args* a, const hop_rotate_grads* g, void* s
 
 size_t hop_attention_scratch_bytes(const hop_attention_args* a) {
     if (!attention_ok(a) || a->q_rows == 0) return 0;
-    return forward_bytes(a, hopa_forward_parts(attention_task(a), a->dtype));
+    HopAttentionTask t = attention_task(a);
+    return hopa_forward_plan(&t, a->dtype, nullptr).bytes;
 }
 
 int hop_attention(const hop_attention_args* a, void* o, int64_t ldo, float* lse, void* scratch, size_t scratch_bytes, void* stream) {
@@ -164,13 +161,10 @@ int hop_attention(const hop_attention_args* a, void* o, int64_t ldo, float* lse,
     HopAttentionTask t = attention_task(a);
     t.o = o; t.ldo = ldo;
     t.lse = lse;
-    t.parts = hopa_forward_parts(t, a->dtype);
-    if (t.parts > 1) {
-        if (scratch_bytes < forward_bytes(a, t.parts)) return HOP_ERR_ARENA_TOO_SMALL;
-        if (!scratch || ((uintptr_t)scratch & 15u)) return HOP_ERR_INVALID_ARG;
-        t.partial = (float*)scratch;
-    }
-    const int rc = hopa_forward(t, a->dtype, stream);
+    const HopAttentionPlan p = hopa_forward_plan(&t, a->dtype, (char*)scratch);
+    if (scratch_bytes < p.bytes) return HOP_ERR_ARENA_TOO_SMALL;
+    if (p.bytes && (!scratch || ((uintptr_t)scratch & 15u))) return HOP_ERR_INVALID_ARG;
+    const int rc = hopa_forward(t, a->dtype, p, stream);
     return rc ? hip_fail((hipError_t)rc, "attention launch") : HOP_OK;
 }
 

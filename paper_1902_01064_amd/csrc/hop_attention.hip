@@ -70,11 +70,11 @@ __global__ __launch_bounds__((FEW ? kFewWaves<T, D> : 4) * 64, (FEW || (sizeof(T
     const bool live = pair < pairs;
     const int row = live ? divide(pair, t.group_inverse) : 0, its = live ? pair - row * t.group : 0;
     const int limit = live ? visible(seq, t.causal, row) : seq.nk;             // keys that the lane's column sees
-    const T* q = (const T*)t.q + (seq.q0 + row) * t.ldq + (head * t.group + its) * t.cols;
-    const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.cols;
-    const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.cols;
+    const T* q = (const T*)t.q + (seq.q0 + row) * t.ldq + (head * t.group + its) * t.head;
+    const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.head;
+    const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.head;
     typename L::frag fq[L::kSteps];
-    load_columns<T, D, FED>(fq, q, t.cols, live);
+    load_columns<T, D, FED>(fq, q, t.head, live);
     auto visible_of = [&](int pair) { return visible(seq, t.causal, divide(pair, t.group_inverse)); };
     const int all_see = visible_of(mine), some_see = mine < pairs ? visible_of(min(mine + 32, pairs) - 1) : 0;
     const int all_see_here = visible_of(first);                                       // of the workgroup's
@@ -83,7 +83,7 @@ __global__ __launch_bounds__((FEW ? kFewWaves<T, D> : 4) * 64, (FEW || (sizeof(T
     const int part_begin = from < seq.nk ? (int)from : seq.nk, begin = part_begin + (FEW ? wave * kRows : 0);
     const int end = min(min(part_begin + whole, seq.nk), visible_of(min(first + (1 << kShift), pairs) - 1));
 
-    const Rows gk = {t.ldk, 1, 0, t.cols}, gv = {t.ldv, 1, 0, t.cols};
+    const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
     Feed<T, D, kRows, NT, FED, false> feed_k, feed_v;
     feed_k.begin(gk, 0);
     feed_v.begin(gv, 0);
@@ -313,15 +313,16 @@ __global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t)
 // Few pairs to a sequence.
 bool few(const HopAttentionTask& t) { return (int64_t)t.q_rows * t.group <= (int64_t)32 * t.S; }
 
-template <typename T, int D, bool FED>
-int launch(const HopAttentionTask& t, hipStream_t stream) {
+template <typename T, int D>
+int launch(const HopAttentionTask& t, bool fed, hipStream_t stream) {
     const int64_t pairs = (int64_t)t.q_rows * t.group;
     if (few(t)) {
-        const int64_t grid = ((pairs + 31) / 32 + t.S) * t.k_heads * t.parts;
-        attention_kernel<T, D, FED, true><<<dim3((unsigned)grid), dim3(kFewWaves<T, D> * 64), 0, stream>>>(t);
+        const dim3 grid((unsigned)(((pairs + 31) / 32 + t.S) * t.k_heads * t.parts)), threads(kFewWaves<T, D> * 64);
+        if (fed) attention_kernel<T, D, true, true><<<grid, threads, 0, stream>>>(t);
+        else attention_kernel<T, D, false, true><<<grid, threads, 0, stream>>>(t);
     } else {
         const int64_t grid = ((pairs + 127) / 128 + t.S) * t.k_heads * t.parts;
-        attention_kernel<T, D, FED, false><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(t);
+        attention_kernel<T, D, true, false><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(t);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && t.parts > 1) {
@@ -332,17 +333,14 @@ int launch(const HopAttentionTask& t, hipStream_t stream) {
 }
 
 template <typename T>
-int launch(const HopAttentionTask& t, hipStream_t stream) {
+int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t stream) {
+    launch_copies<T>(plan.copies, stream);
     auto fits = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && (ld * sizeof(T)) % 16 == 0; };
-    const bool fed = fits(t.q, t.ldq) && fits(t.k, t.ldk) && fits(t.v, t.ldv) && (t.cols * sizeof(T)) % 16 == 0;
-    if (t.cols <= 64) return fed ? launch<T, 64, true>(t, stream) : launch<T, 64, false>(t, stream);
-    return fed ? launch<T, 128, true>(t, stream) : launch<T, 128, false>(t, stream);
+    const bool fed = fits(t.q, t.ldq) && fits(t.k, t.ldk) && fits(t.v, t.ldv) && (t.head * sizeof(T)) % 16 == 0;
+    return t.cols <= 64 ? launch<T, 64>(t, fed, stream) : launch<T, 128>(t, fed, stream);
 }
 
-}  // namespace
-
-int hopa_forward_parts(const HopAttentionTask& t, int dtype) {
-    (void)dtype;
+int parts_of(const HopAttentionTask& t) {
     const int64_t step = few(t) ? 32 : 128, tiles = (((int64_t)t.q_rows * t.group + step - 1) / step + t.S) * t.k_heads, keys = t.k_rows / t.S;
     // Workgroups, and keys of a part: with few pairs a workgroup to a CU (the next token of 32 sequences of 2048 tokens, 32 heads on 8 of 128: 46.5 us, with two 54), and no parts where
     // its wavefronts have little to do (4000 keys in parts of 512 16 us, of 1024 20).
@@ -350,6 +348,24 @@ int hopa_forward_parts(const HopAttentionTask& t, int dtype) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((wanted + tiles - 1) / tiles, keys / least), 64));
 }
 
-int hopa_forward(const HopAttentionTask& t, int dtype, void* stream) {
-    return dtype == HOP_BF16 ? launch<bf16>(t, (hipStream_t)stream) : launch<float>(t, (hipStream_t)stream);
+}  // namespace
+
+HopAttentionPlan hopa_forward_plan(HopAttentionTask* task, int dtype, char* scratch) {
+    HopAttentionTask& t = *task;
+    HopAttentionPlan p = {};
+    Planner planner(task, &p, dtype, scratch);
+    const int heads = t.k_heads * t.group;
+    t.parts = parts_of(t);
+    if (t.parts > 1) t.partial = (float*)planner.take((size_t)t.parts * t.q_rows * heads * (t.cols + 2) * 4);
+    // Few queries read a key once, and that is all their time: they fill tiles from rows that are not aligned through registers.
+    if (!few(t)) {
+        planner.align(t.q, t.ldq, t.q_rows, heads, t.q_begin);
+        planner.align(t.k, t.ldk, t.k_rows, t.k_heads, t.k_begin);
+        planner.align(t.v, t.ldv, t.k_rows, t.k_heads, t.k_begin);
+    }
+    return p;
+}
+
+int hopa_forward(const HopAttentionTask& t, int dtype, const HopAttentionPlan& plan, void* stream) {
+    return dtype == HOP_BF16 ? launch<bf16>(t, plan, (hipStream_t)stream) : launch<float>(t, plan, (hipStream_t)stream);
 }

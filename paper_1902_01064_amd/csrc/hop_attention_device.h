@@ -239,6 +239,70 @@ struct Feed {
     }
 };
 
+// ---- rows that the memory unit cannot take, laid out anew -----------------------------------------
+// It fills tiles 16 bytes at a time, from addresses that are multiples of them.  Matrices whose rows or heads are not get a copy with heads of whole 16 bytes (zeros
+// at the end): read and written once, in one launch, beside the passes over them that follow.
+namespace {
+template <typename T>
+__global__ __launch_bounds__(256) void attention_align_kernel(HopAttentionCopies c) {
+    typedef Tile<T, 64> L;                      // of which only the chunks matter
+    const auto& m = c.of[blockIdx.y];
+    const int chunks = c.head / L::kChunk, per_row = m.heads * chunks;
+    int b = 0, e = m.rows;
+    if (m.begin) {
+        b = clamp_int(((const HOPL_GLOBAL int32_t*)m.begin)[0], 0, m.rows);
+        e = clamp_int(((const HOPL_GLOBAL int32_t*)m.begin)[c.S], b, m.rows);
+    }
+    const int64_t all = (int64_t)(e - b) * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = b + i / per_row;
+        const int at = (int)(i % per_row), head = at / chunks, column = at % chunks * L::kChunk, n = c.cols - column;
+        const T* from = (const T*)m.from + row * m.ld + head * c.cols + column;
+        typename L::frag v;
+        if (n >= L::kChunk) v = *(const HOPL_GLOBAL typename L::frag_any*)from;
+        else v = load_short<typename L::frag>(from, n);
+        *(HOPL_GLOBAL typename L::frag*)((T*)m.to + row * m.heads * c.head + head * c.head + column) = v;
+    }
+}
+template <typename T>
+void launch_copies(const HopAttentionCopies& c, hipStream_t stream) {
+    if (!c.n) return;
+    int64_t most = 1;
+    for (int i = 0; i < c.n; ++i) {
+        const int64_t blocks = ((int64_t)c.of[i].rows * c.of[i].heads * c.head * (int64_t)sizeof(T) / 16 + 255) / 256;
+        most = most < blocks ? blocks : most;
+    }
+    attention_align_kernel<T><<<dim3((unsigned)(most < 2048 ? most : 2048), (unsigned)c.n), dim3(256), 0, stream>>>(c);
+}
+}  // namespace
+struct Planner {
+    HopAttentionTask& t;
+    HopAttentionPlan& p;
+    char* scratch;
+    int elem;
+    Planner(HopAttentionTask* task, HopAttentionPlan* plan, int dtype, char* scratch_) : t(*task), p(*plan), scratch(scratch_), elem(dtype == HOP_BF16 ? 2 : 4) {
+        t.head = p.copies.cols = t.cols;
+        p.copies.S = t.S;
+    }
+    char* take(size_t bytes) {
+        char* at = (char*)((uintptr_t)scratch + p.bytes);
+        p.bytes += (bytes + 255) / 256 * 256;
+        return at;
+    }
+    bool fits(const void* m, int64_t ld) const { return ((uintptr_t)m & 15u) == 0 && (ld * elem) % 16 == 0 && (t.cols * elem) % 16 == 0; }
+    // a pointer of the task's and its distance
+    template <typename P>
+    void align(P& m, int64_t& ld, int rows, int heads, const int32_t* begin) {
+        auto& c = p.copies;
+        t.head = c.head = (t.cols * elem + 15) / 16 * 16 / elem;
+        if (!rows || fits(m, ld)) return;
+        char* to = take((size_t)rows * heads * t.head * elem);
+        c.of[c.n++] = {m, to, ld, begin, rows, heads};
+        m = to;
+        ld = (int64_t)heads * t.head;
+    }
+};
+
 // A lane's column of the second operand: its row's chunks 2 step + lane / 32, zeros where there is no row.
 template <typename T, int D, bool FED>
 __device__ __forceinline__ void load_columns(typename Tile<T, D>::frag* to, const T* row, int cols, bool live) {

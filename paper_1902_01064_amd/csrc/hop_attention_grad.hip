@@ -615,31 +615,6 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTa
     else join_tile<T, false>(t, most);
 }
 
-// ---- rows that the memory unit cannot take, laid out anew -----------------------------------------
-// It fills tiles 16 bytes at a time, from addresses that are multiples of them.  Matrices whose rows or heads are not get a copy with heads of whole 16 bytes (zeros
-// at the end): read and written once, in one launch, beside two passes over them that follow.
-template <typename T>
-__global__ __launch_bounds__(256) void attention_align_kernel(HopAttentionCopies c) {
-    typedef Tile<T, 64> L;                      // of which only the chunks matter
-    const auto& m = c.of[blockIdx.y];
-    const int chunks = c.head / L::kChunk, per_row = m.heads * chunks;
-    int b = 0, e = m.rows;
-    if (m.begin) {
-        b = clamp_int(((const HOPL_GLOBAL int32_t*)m.begin)[0], 0, m.rows);
-        e = clamp_int(((const HOPL_GLOBAL int32_t*)m.begin)[c.S], b, m.rows);
-    }
-    const int64_t all = (int64_t)(e - b) * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = b + i / per_row;
-        const int at = (int)(i % per_row), head = at / chunks, column = at % chunks * L::kChunk, n = c.cols - column;
-        const T* from = (const T*)m.from + row * m.ld + head * c.cols + column;
-        typename L::frag v;
-        if (n >= L::kChunk) v = *(const HOPL_GLOBAL typename L::frag_any*)from;
-        else v = load_short<typename L::frag>(from, n);
-        *(HOPL_GLOBAL typename L::frag*)((T*)m.to + row * m.heads * c.head + head * c.head + column) = v;
-    }
-}
-
 template <typename T, int D>
 int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t stream) {
     constexpr int grid = kCus, kThreads = 256 * kHalves<T, D>, kJoins = (kCus - 1) * (kTile / 8);
@@ -651,13 +626,8 @@ int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t 
 }
 
 template <typename T>
-int launch(HopAttentionTask t, const HopAttentionPlan& plan, hipStream_t stream) {
-    if (plan.copies.n) {
-        int64_t most = 1;
-        for (int i = 0; i < plan.copies.n; ++i)
-            most = std::max<int64_t>(most, ((int64_t)plan.copies.of[i].rows * plan.copies.of[i].heads * plan.copies.head * sizeof(T) / 16 + 255) / 256);
-        attention_align_kernel<T><<<dim3((unsigned)std::min<int64_t>(most, 2048), (unsigned)plan.copies.n), dim3(256), 0, stream>>>(plan.copies);
-    }
+int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t stream) {
+    launch_copies<T>(plan.copies, stream);
     return t.cols <= 64 ? launch<T, 64>(t, plan, stream) : launch<T, 128>(t, plan, stream);
 }
 
@@ -666,39 +636,20 @@ int launch(HopAttentionTask t, const HopAttentionPlan& plan, hipStream_t stream)
 HopAttentionPlan hopa_grad_plan(HopAttentionTask* task, int dtype, char* scratch) {
     HopAttentionTask& t = *task;
     HopAttentionPlan p = {};
+    Planner planner(task, &p, dtype, scratch);
     p.q_tiles = ((int64_t)t.q_rows * t.group + kTile - 1) / kTile + t.S;
     p.k_tiles = ((int64_t)t.k_rows + kTile - 1) / kTile + t.S;
-    auto take = [&](size_t bytes) {
-        char* at = (char*)((uintptr_t)scratch + p.bytes);           // scratch is null where only the bytes are asked for
-        p.bytes += (bytes + 255) / 256 * 256;
-        return at;
-    };
     auto plan_bytes = [](int64_t tiles) { return sizeof(Plan) + tiles * sizeof(PlanTile); };
-    t.terms = (float*)take((size_t)2 * t.k_heads * t.group * t.q_rows * 4);
-    t.q_plan = take(plan_bytes(p.q_tiles));
-    t.k_plan = take(plan_bytes(p.k_tiles));
-    t.partial = (float*)take((size_t)kCus * 2 * 3 * kTile * t.cols * 4);          // two parts of a workgroup, of dq, dk and dv
-    // copies of what the memory unit cannot take
-    const int elem = dtype == HOP_BF16 ? 2 : 4, chunk = 16 / elem, head = (t.cols + chunk - 1) / chunk * chunk;
-    auto fits = [&](const void* m, int64_t ld) { return ((uintptr_t)m & 15u) == 0 && (ld * elem) % 16 == 0; };
-    auto& c = p.copies;
-    t.head = head;
-    c.cols = t.cols;
-    c.head = head;
-    c.S = t.S;
-    auto align = [&](auto& m, int64_t& ld, int rows, int heads, const int32_t* begin) {
-        if (!rows || (head == t.cols && fits(m, ld))) return;
-        char* to = take((size_t)rows * heads * head * elem);
-        c.of[c.n++] = {m, to, ld, begin, rows, heads};
-        m = to;
-        ld = (int64_t)heads * head;
-    };
     const int heads = t.k_heads * t.group;
-    align(t.q, t.ldq, t.q_rows, heads, t.q_begin);
-    align(t.grad, t.ldgrad, t.q_rows, heads, t.q_begin);
-    align(t.o, t.ldo, t.q_rows, heads, t.q_begin);
-    align(t.k, t.ldk, t.k_rows, t.k_heads, t.k_begin);
-    align(t.v, t.ldv, t.k_rows, t.k_heads, t.k_begin);
+    t.terms = (float*)planner.take((size_t)2 * heads * t.q_rows * 4);
+    t.q_plan = planner.take(plan_bytes(p.q_tiles));
+    t.k_plan = planner.take(plan_bytes(p.k_tiles));
+    t.partial = (float*)planner.take((size_t)kCus * 2 * 3 * kTile * t.cols * 4);          // two parts of a workgroup, of dq, dk and dv
+    planner.align(t.q, t.ldq, t.q_rows, heads, t.q_begin);
+    planner.align(t.grad, t.ldgrad, t.q_rows, heads, t.q_begin);
+    planner.align(t.o, t.ldo, t.q_rows, heads, t.q_begin);
+    planner.align(t.k, t.ldk, t.k_rows, t.k_heads, t.k_begin);
+    planner.align(t.v, t.ldv, t.k_rows, t.k_heads, t.k_begin);
     return p;
 }
 

@@ -13,7 +13,7 @@ struct HopAttentionTask {
     const int32_t *q_begin, *k_begin;      // null: one sequence of all rows
     int32_t S, q_rows, k_rows;
     int32_t k_heads, group, cols;          // group: query heads of a key head
-    int32_t head;                          // gradient: columns from a head to the next one where q, k, v, o and grad are read
+    int32_t head;                          // columns from a head to the next one where q, k, v, o and grad are read
     uint32_t group_inverse;                // ceil(2^32 / group), 0 for 1
     int32_t causal, parts;
     float scale, scale_log2;               // scale_log2 = scale log2(e)
@@ -31,7 +31,7 @@ struct HopAttentionTask {
     void *q_plan, *k_plan;                 // how pairs and keys are shared out
 };
 
-// Matrices that the gradient copies first, each to rows of `heads` heads `head` columns apart.
+// Matrices that are copied first, each to rows of `heads` heads `head` columns apart.
 struct HopAttentionCopies {
     struct {
         const void* from;
@@ -42,11 +42,11 @@ struct HopAttentionCopies {
     } of[5];
     int32_t n, cols, head, S;
 };
-// What the gradient needs besides its task: most tiles of pairs and keys, copies to make, bytes of scratch.
+// What a call needs besides its task: copies to make, bytes of scratch, most tiles of the gradient's pairs and keys.
 struct HopAttentionPlan {
-    int64_t q_tiles, k_tiles;
     HopAttentionCopies copies;
     size_t bytes;
+    int64_t q_tiles, k_tiles;
 };
 
 struct HopRotateTask {
@@ -67,9 +67,10 @@ struct HopRotateTask {
     double turns[HOP_MAX_HEAD_COLS / 2];   // a pair's turns per position: base^(-2 i / rotary) / (2 pi)
 };
 
-int hopa_forward_parts(const HopAttentionTask& t, int dtype);
-int hopa_forward(const HopAttentionTask& t, int dtype, void* stream);
-HopAttentionPlan hopa_grad_plan(HopAttentionTask* t, int dtype, char* scratch);           // sets t's parts of the scratch and what is read instead of its matrices
+// They set the task's parts of the scratch (null: only the bytes are asked for) and what is read instead of its matrices.
+HopAttentionPlan hopa_forward_plan(HopAttentionTask* t, int dtype, char* scratch);
+HopAttentionPlan hopa_grad_plan(HopAttentionTask* t, int dtype, char* scratch);
+int hopa_forward(const HopAttentionTask& t, int dtype, const HopAttentionPlan& plan, void* stream);
 int hopa_grad(const HopAttentionTask& t, int dtype, const HopAttentionPlan& plan, void* stream);
 
 int hopa_rotate(const HopRotateTask& t, int dtype, const HopIndex& index, void* stream);

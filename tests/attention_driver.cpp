@@ -31,8 +31,14 @@ void rotate_ok(const HopRotateTask& t) {
 }
 }  // namespace
 
-int hopa_forward_parts(const HopAttentionTask& t, int) { return t.k_rows > 64 ? 3 : 1; }
-int hopa_forward(const HopAttentionTask& t, int, void*) {
+HopAttentionPlan hopa_forward_plan(HopAttentionTask* t, int, char* scratch) {
+    HopAttentionPlan p = {};
+    t->parts = t->k_rows > 64 ? 3 : 1;
+    p.bytes = t->parts > 1 ? 512 : 0;
+    t->partial = t->parts > 1 ? (float*)scratch : nullptr;
+    return p;
+}
+int hopa_forward(const HopAttentionTask& t, int, const HopAttentionPlan&, void*) {
     attention_ok(t);
     require(t.q_rows > 0 && t.o && (t.parts == 1) == !t.partial, "attention");
     return ++launches, 0;
