@@ -21,6 +21,8 @@ namespace {
 
 constexpr int kShift = 7, kTile = 1 << kShift;          // pairs or keys of a tile, 32 of a wavefront
 constexpr int kCus = 256;
+// kSkip: units that a wavefront's columns see nothing of are left out in fp32, whose products take long (32 sequences of 128 rows: 99 us, with them 103); in bfloat16 the other
+// wavefronts of the stage decide and the branch costs more than it saves (8192 rows, causal: 1003 us, without it 960).
 constexpr int kExact = 128;                             // keys: see attention_dq_kernel
 // Two halves of a workgroup with the same tile take every other 32 rows of a stage, so that a SIMD has two wavefronts, of which one computes while the other waits, and the CU
 // only one set of tiles (one wavefront with twice the registers issues an instruction every 5 cycles at best, which is too few beside its products: 1860 us for the above).  In fp32 with 128 columns the sums and operands of one wavefront fill a SIMD's registers.
@@ -159,6 +161,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
     typedef Weights<T> W;
     constexpr int kH = kHalves<T, D>, NT = 256 * kH, kRows = 32 * kH, kBytes = kRows * L::kLine, kU = D / 32, kS = L::kSteps;
     constexpr int kStage = 2 * kBytes;                      // keys, values
+    constexpr bool kSkip = sizeof(T) == 4;
     __shared__ __attribute__((aligned(16))) char pool[2 * kStage];
     __shared__ int not_finite;
     __shared__ float exact[2][kTile];
@@ -185,7 +188,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
 
         const int limit = live ? visible(its_rows, t.causal, row) : seq.nk;
         auto visible_of = [&](int p) { return visible(its_rows, t.causal, divide(p, t.group_inverse)); };
-        const int all_see = visible_of(min(mine, pairs - 1)), all_see_here = visible_of(first);
+        const int all_see = visible_of(min(mine, pairs - 1)), all_see_here = visible_of(first), some_see = mine < pairs ? visible_of(min(mine + 32, pairs) - 1) : 0;
         const int end = min(visible_of(min(first + kTile, pairs) - 1), last_stage * kRows), begin = first_stage * kRows;
 
         const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
@@ -271,6 +274,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         auto work = [&](const char* b, int i) __attribute__((always_inline)) {
             const Places<T, D> places = all_places.again();
             const int key = begin + i * kRows + 32 * half;
+            if (kSkip && key >= some_see) return;                      // all of it is hidden from the wavefront's pairs
             const char* sk = b + 32 * half * L::kLine;
             const char* sv = sk + kBytes;
             constexpr int kN = 2 * kS + 2 * kU, kAhead = sizeof(T) == 4 ? 2 : 4, kFrom = kS + (sizeof(T) == 4 ? 1 : 2);
@@ -359,6 +363,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
     typedef Tile<T, D> L;
     typedef Weights<T> W;
     constexpr int kH = kHalves<T, D>, NT = 256 * kH, kRows = 32 * kH, kBytes = kRows * L::kLine, kS = L::kSteps;
+    constexpr bool kSkip = sizeof(T) == 4;
     constexpr int kStage = 2 * kBytes + 512;                // queries, gradients, lse log2(e) of the pairs, their D
     // Both sums of 128 columns leave no registers for the keys and values: there they wait in LDS.
     constexpr bool kHeld = kH == 1 || D * sizeof(T) <= 128;
@@ -388,6 +393,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         const float* terms = t.terms + head * pairs_of(t) + (int64_t)seq.q0 * t.group;
 
         const int least = live ? seen_from(t, seq.nq, seq.nk, key) : 0;
+        const int some_see = mine < seq.nk ? seen_from(t, seq.nq, seq.nk, mine) : pairs;
         const int all_see = seen_from(t, seq.nq, seq.nk, min(mine + 32, seq.nk) - 1), all_see_here = seen_from(t, seq.nq, seq.nk, min(first + kTile, seq.nk) - 1);
         const int start = min(pairs, seen_from(t, seq.nq, seq.nk, first) / kRows * kRows);
         const int begin = start + first_stage * kRows, end = min(pairs, start + last_stage * kRows);
@@ -442,6 +448,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             Places<T, D> places = all_places.again();
             if constexpr (kCuts > 1) places.across ^= cut * kSumCols * (int)sizeof(T);
             const int pair = begin + i * kRows + 32 * half;
+            if (kSkip && pair + 32 <= some_see) return;                // all of it is hidden from the wavefront's keys
             const char* sq = b + 32 * half * L::kLine;
             const char* sg = sq + kBytes;
             const char* st = b + 2 * kBytes + 128 * half + 16 * hi;
@@ -487,10 +494,14 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             if (pair < all_see) {
                 asm volatile("");              // a branch, as above
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const bool here = pair + 8 * (r >> 2) + 4 * hi + (r & 3) >= least;
-                    ds[r] = here ? p[r] * (ds[r] - *(const float*)(sd + 32 * (r >> 2) + 4 * (r & 3))) : 0.f;
-                    p[r] = here ? p[r] : 0.f;
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 less = *(const f32x4*)(sd + 32 * i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool here = pair + 8 * i + 4 * hi + e >= least;
+                        ds[4 * i + e] = here ? p[4 * i + e] * (ds[4 * i + e] - less[e]) : 0.f;
+                        p[4 * i + e] = here ? p[4 * i + e] : 0.f;
+                    }
                 }
                 wp = W(p);
 #pragma unroll
@@ -569,10 +580,11 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
 }
 
 // ---- parts, joined in their order -------------------------------------------------------------
-// 8 rows of the tile in which run number blockIdx.x / 16 + 1 begins, if it is the first one to do so.  A part is `sums` matrices: dq, or dk and dv.
+// kJoinRows rows of the tile in which run number blockIdx.x / (kTile / kJoinRows) + 1 begins, if it is the first one to do so.  A part is `sums` matrices: dq, or dk and dv.
+constexpr int kJoinRows = 32;
 template <typename T, bool KEYS>
 __device__ __forceinline__ void join_tile(const HopAttentionTask& t, int most) {
-    constexpr int kSums = KEYS ? 2 : 1, kEach = 8;
+    constexpr int kSums = KEYS ? 2 : 1, kEach = kJoinRows;
     const Runs runs(KEYS ? t.k_plan : t.q_plan, t.k_heads, most);
     const int64_t run = blockIdx.x / (kTile / kEach) + 1, tiles = runs.plan->tiles;
     if (run >= runs.blocks) return;
@@ -617,7 +629,7 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(HopAttentionTa
 
 template <typename T, int D>
 int launch(const HopAttentionTask& t, const HopAttentionPlan& plan, hipStream_t stream) {
-    constexpr int grid = kCus, kThreads = 256 * kHalves<T, D>, kJoins = (kCus - 1) * (kTile / 8);
+    constexpr int grid = kCus, kThreads = 256 * kHalves<T, D>, kJoins = (kCus - 1) * (kTile / kJoinRows);
     attention_plan_kernel<<<dim3(2), dim3(kPlanners), 0, stream>>>(t, 32 * kHalves<T, D>, plan.q_tiles, plan.k_tiles);
     if (t.q_rows) attention_dq_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
     if (t.k_rows) attention_dkv_kernel<T, D><<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
