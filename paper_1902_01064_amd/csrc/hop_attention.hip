@@ -46,7 +46,7 @@ __global__ __launch_bounds__((FEW ? kFewWaves<T, D> : 4) * 64, (FEW || (sizeof(T
     __shared__ __attribute__((aligned(16))) char all_k0[kAll], all_v0[kAll], all_k1[kAll], all_v1[kAll];
     const int head = blockIdx.x % t.k_heads, rest = blockIdx.x / t.k_heads, part = rest % t.parts;
     int s, first;
-    if (!find_tile<true>(t.q_begin, t.S, t.q_rows, t.group, kShift, rest / t.parts, &s, &first)) return;
+    if (!find_tile(t.q_begin, t.S, t.q_rows, t.group, kShift, rest / t.parts, &s, &first)) return;
     const Sequence seq = sequence(t, s);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hi = lane >> 5;
     const int pairs = seq.nq * t.group, mine = first + (FEW ? 0 : wave * 32);            // the wavefront's first pair

@@ -432,9 +432,8 @@ __device__ __forceinline__ void rows_of(const int32_t* begin, int s, int rows, i
 }
 
 // Tile number `tile` of the sequences' rows, 1 << shift (times `by` a row) to a tile: its sequence and first row (or pair).  False: there are fewer.
-// Every wavefront works it out for itself, 64 sequences at a time.  DEEP: within 64 sequences in the order of the place in the sequence, the farthest first; where queries
+// Every wavefront works it out for itself, 64 sequences at a time, and within those in the order of the place in the sequence, the farthest first: where queries
 // see what is in front of them those have most to do, and what begins last is to be short.
-template <bool DEEP>
 __device__ __forceinline__ bool find_tile(const int32_t* begin, int S, int rows, int by, int shift, int tile, int* s, int* first) {
     const int lane = threadIdx.x & 63, step = 1 << shift;
     int seen = 0;
@@ -453,14 +452,14 @@ __device__ __forceinline__ bool find_tile(const int32_t* begin, int S, int rows,
             seen += all;
             continue;
         }
-        if (!DEEP || S == 1) {
+        if (S == 1) {
             const uint64_t behind = __ballot(seen + scan > tile);
             if (!behind) return false;                        // only where a broken table made the sums overflow
             const int l = __builtin_ctzll(behind), its = __builtin_amdgcn_readlane(tiles, l);
             const int at = tile - (seen + __builtin_amdgcn_readlane(scan, l) - its);
             if (at < 0 || at >= its) return false;
             *s = base + l;
-            *first = (DEEP ? its - 1 - at : at) << shift;
+            *first = (its - 1 - at) << shift;
             return true;
         }
         // the deepest place from which on there are more tiles than that

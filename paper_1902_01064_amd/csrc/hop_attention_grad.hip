@@ -6,7 +6,7 @@
 // Two kernels, each with sums of its own in registers, so that results are the same bits every time: one passes over the keys of a tile of pairs for dq
 // (and leaves D and lse for the other), one over the pairs of a tile of keys for dk and dv.  The price is that scores and do v^T are computed
 // twice: 14 operations where 10 would do.  Both take even shares of all tiles, which a small kernel in front of them lays out from the tables: with a workgroup to a tile
-// the longest sequence's tiles decided (12288 tokens in 6 sequences, 16 heads on 2: 1076 us, now 467).
+// the longest sequence's tiles decided (12288 tokens in 6 sequences, 16 heads on 2: 1076 us, now 458).
 //
 // What bounds them is the matrix unit, at the clock that its power leaves: 8192 tokens that all see each other, 16 heads of 128 columns on 2, bfloat16, take 1716 us,
 // 1120 TFLOP/s of the 14 operations (a large library product reaches 1230 to 1390 on such numbers); 58 % of the cycles have a product under way.
@@ -37,7 +37,7 @@ __device__ __forceinline__ int seen_from(const HopAttentionTask& t, int nq, int 
 // A workgroup for the tiles of pairs, one for those of keys.  `rows`: of a stage.
 constexpr int kPlanners = 1024;
 // What a tile takes beside its stages, in stages: 17500 cycles for pairs, of which a stage of 128 columns in bfloat16 takes 2440, and more for keys.  12288 tokens, 16 heads on 2:
-// dq and dk, dv in 211 and 250 us; as if a tile took nothing 439 and 272.
+// dq and dk, dv in 215 and 237 us; as if a tile took nothing 439 and 272.
 constexpr int kPairsFixed = 8, kKeysFixed = 10;
 __device__ __forceinline__ int64_t scan_all(int64_t v, int64_t* waves, int64_t* all) {          // sum of those in front
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
