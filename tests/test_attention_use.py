@@ -21,11 +21,18 @@ def made(seed, rows, cols, dtype):
 
 # Many sequences of any lengths, so that tiles are cut between workgroups in every way: each row against the 64-bit statement.
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("S,longest,hq,hk,D,causal", [(300, 40, 3, 1, 16, True), (70, 200, 2, 2, 64, False), (5, 900, 2, 1, 72, True), (2, 1500, 4, 1, 128, True), (1, 3000, 1, 1, 32, True)])
+@pytest.mark.parametrize("S,longest,hq,hk,D,causal", [(300, 40, 3, 1, 16, True), (70, 200, 2, 2, 64, False), (5, 900, 2, 1, 72, True), (2, 1500, 4, 1, 128, True), (1, 3000, 1, 1, 32, True),
+                                                      (4096, 3, 1, 1, 8, True)])
 def test_many_lengths(dtype, S, longest, hq, hk, D, causal):
     r = np.random.default_rng(S)
     n = [int(v) for v in r.integers(0, longest + 1, S)]
     check(dtype, n, n, hq, hk, D, causal)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,hk", [(1024, 1024), (1024, 1), (1023, 341)])
+def test_as_many_heads_as_there_may_be(dtype, hq, hk):
+    check(dtype, [3, 1], [5, 40], hq, hk, 4, True, odd=True)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
