@@ -43,7 +43,11 @@ HopRotateTask rotate_task(const hop_rotate_args* a) {
     t.inv_cols = (float)(1.0 / a->cols);
     t.q_weight = a->q_weight; t.k_weight = a->k_weight;
     t.q_stride = a->q_weight_stride; t.k_stride = a->k_weight_stride;
-    for (int i = 0; i < a->rotary / 2; ++i) t.turns[i] = std::pow(a->base, -2.0 * i / a->rotary) / kTwoPi;
+    // base^(-2 i / rotary) as products of eight and eight powers, a rounding more of 64 bits: 64 powers are 0.3 us of a call of 9.7
+    double near[8], far[8];
+    for (int i = 0; i < 8 && i < a->rotary / 2; ++i) near[i] = std::pow(a->base, -2.0 * i / a->rotary) / kTwoPi;
+    for (int i = 0; 8 * i < a->rotary / 2; ++i) far[i] = std::pow(a->base, -16.0 * i / a->rotary);
+    for (int i = 0; i < a->rotary / 2; ++i) t.turns[i] = near[i % 8] * far[i / 8];
     return t;
 }
 bool rotate_grads_ok(const hop_rotate_args* a, const hop_rotate_grads* g) {
