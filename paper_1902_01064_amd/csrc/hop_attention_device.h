@@ -522,11 +522,10 @@ __device__ __forceinline__ void stage(char* __restrict now, char* __restrict nex
     work(now, i);
 }
 // The first one is issued beforehand, behind a barrier with whoever still reads from the buffers.
-template <typename ISSUE, typename PUT, typename WORK>
-__device__ __forceinline__ void stages(int n, char* pool, int bytes, ISSUE issue, PUT put, WORK work) {
+template <typename ISSUE, typename WORK>
+__device__ __forceinline__ void stages(int n, char* pool, int bytes, ISSUE issue, WORK work) {
     char *now = pool, *next = pool + bytes;
     for (int i = 0; i < n; ++i) {
-        put(now);
         arrive();                               // this stage is there, and nobody reads from the one before any more
         stage(now, next, i, n, issue, work);
         char* const other = now;

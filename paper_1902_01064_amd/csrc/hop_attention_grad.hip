@@ -243,7 +243,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         // With few keys to a query o's rounding weighs: D once more, as sum_j p_ij do_i v_j, which is exact to fp32's rounding and costs these tiles two products more.
         if (sizeof(T) == 2 && n && seq.stages * kRows <= kExact) {
             float sum = 0.f;
-            stages(n, pool, kStage, issue, [](char*) {}, [&](const char* b, int i) __attribute__((always_inline)) {
+            stages(n, pool, kStage, issue, [&](const char* b, int i) __attribute__((always_inline)) {
                 const int key = i * kRows + 32 * half;
                 const char* sk = b + 32 * half * L::kLine;
                 f32x16 p = (f32x16)(0.f), g = (f32x16)(0.f);
@@ -327,7 +327,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             for (int c = 0; c < kU; ++c) dq[c] = (f32x16)(0.f);
         };
         clear();
-        if (n) stages(n, pool, kStage, issue, [](char*) {}, work);
+        if (n) stages(n, pool, kStage, issue, work);
         if (!n) __syncthreads();                           // the stages have theirs
         if (t.causal && live && !all_finite(dq)) not_finite = 1;
         __syncthreads();
@@ -538,7 +538,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
                 if (n) issue(pool, 0);
             }
             clear();
-            if (n) stages(n, pool, kStage, issue, [](char*) {}, work);
+            if (n) stages(n, pool, kStage, issue, work);
             if (!n) __syncthreads();                       // the stages have theirs
             if (t.causal && live && !(all_finite(dk) && all_finite(dv))) not_finite = 1;
             __syncthreads();
