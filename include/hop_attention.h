@@ -25,7 +25,7 @@
  *  - Results may not overlap what a call reads, except where it is said.
  *  - Sizes: heads of up to HOP_MAX_HEAD_COLS columns, rows times query heads below 2^30, distances between rows up to 2^22 elements, up to
  *    HOP_MAX_GROUPS sequences.  Fastest are heads of 64 and 128 columns in rows whose addresses and distances are multiples of 16 bytes; others
- *    are copied into the scratch first, except where a few queries read long keys.
+ *    are copied into the scratch first, except where a few queries read the keys of bfloat16 rows, or of fp32 heads of up to 64 columns.
  */
 #ifndef HOP_ATTENTION_H
 #define HOP_ATTENTION_H

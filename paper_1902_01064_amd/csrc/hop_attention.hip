@@ -313,13 +313,22 @@ __global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t)
 // Few pairs to a sequence.
 bool few(const HopAttentionTask& t) { return (int64_t)t.q_rows * t.group <= (int64_t)32 * t.S; }
 
+// Few queries read a key once, and that is all their time: they fill tiles from rows that are not aligned through registers, and others' rows are copied first.
+// In fp32 tiles of 128 columns and what is on its way to them are more than all registers (172 bytes of scratch a lane), so there rows are copied for few queries too.
+template <typename T, int D>
+constexpr bool kThroughRegisters = D * (int)sizeof(T) <= 256;
+
 template <typename T, int D>
 int launch(const HopAttentionTask& t, bool fed, hipStream_t stream) {
     const int64_t pairs = (int64_t)t.q_rows * t.group;
     if (few(t)) {
         const dim3 grid((unsigned)(((pairs + 31) / 32 + t.S) * t.k_heads * t.parts)), threads(kFewWaves<T, D> * 64);
-        if (fed) attention_kernel<T, D, true, true><<<grid, threads, 0, stream>>>(t);
-        else attention_kernel<T, D, false, true><<<grid, threads, 0, stream>>>(t);
+        if constexpr (kThroughRegisters<T, D>) {
+            if (fed) attention_kernel<T, D, true, true><<<grid, threads, 0, stream>>>(t);
+            else attention_kernel<T, D, false, true><<<grid, threads, 0, stream>>>(t);
+        } else {
+            attention_kernel<T, D, true, true><<<grid, threads, 0, stream>>>(t);
+        }
     } else {
         const int64_t grid = ((pairs + 127) / 128 + t.S) * t.k_heads * t.parts;
         attention_kernel<T, D, true, false><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(t);
@@ -357,8 +366,8 @@ HopAttentionPlan hopa_forward_plan(HopAttentionTask* task, int dtype, char* scra
     const int heads = t.k_heads * t.group;
     t.parts = parts_of(t);
     if (t.parts > 1) t.partial = (float*)planner.take((size_t)t.parts * t.q_rows * heads * (t.cols + 2) * 4);
-    // Few queries read a key once, and that is all their time: they fill tiles from rows that are not aligned through registers.
-    if (!few(t)) {
+    const bool through_registers = t.cols <= 64 || (dtype == HOP_BF16 ? kThroughRegisters<bf16, 128> : kThroughRegisters<float, 128>);
+    if (!few(t) || !through_registers) {
         planner.align(t.q, t.ldq, t.q_rows, heads, t.q_begin);
         planner.align(t.k, t.ldk, t.k_rows, t.k_heads, t.k_begin);
         planner.align(t.v, t.ldv, t.k_rows, t.k_heads, t.k_begin);
