@@ -81,7 +81,8 @@ HopAttentionTask attention_task(const hop_attention_args* a) {
     t.S = a->S;
     t.q_rows = (int32_t)a->q_rows; t.k_rows = (int32_t)a->k_rows;
     t.k_heads = a->k_heads; t.group = a->q_heads / a->k_heads; t.cols = a->cols;
-    t.group_inverse = t.group == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + t.group - 1) / t.group);
+    t.group_inverse = hopa_group_inverse(t.group);
+    t.group_shift = hopa_group_shift(t.group);
     t.causal = a->causal; t.parts = 1;
     t.scale = a->scale;
     t.scale_log2 = (float)(a->scale * 1.4426950408889634074);

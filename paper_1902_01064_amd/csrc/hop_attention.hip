@@ -68,14 +68,14 @@ __global__ __launch_bounds__((FEW ? kFewWaves<T, D> : 4) * 64, (FEW || (sizeof(T
     };
     const int pair = mine + (lane & 31);
     const bool live = pair < pairs;
-    const int row = live ? divide(pair, t.group_inverse) : 0, its = live ? pair - row * t.group : 0;
+    const int row = live ? hopa_divide(pair, t.group_inverse, t.group_shift) : 0, its = live ? pair - row * t.group : 0;
     const int limit = live ? visible(seq, t.causal, row) : seq.nk;             // keys that the lane's column sees
     const T* q = (const T*)t.q + (seq.q0 + row) * t.ldq + (head * t.group + its) * t.head;
     const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.head;
     const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.head;
     typename L::frag fq[L::kSteps];
     load_columns<T, D, FED>(fq, q, t.head, live);
-    auto visible_of = [&](int pair) { return visible(seq, t.causal, divide(pair, t.group_inverse)); };
+    auto visible_of = [&](int pair) { return visible(seq, t.causal, hopa_divide(pair, t.group_inverse, t.group_shift)); };
     const int all_see = visible_of(mine), some_see = mine < pairs ? visible_of(min(mine + 32, pairs) - 1) : 0;
     const int all_see_here = visible_of(first);                                       // of the workgroup's
     const int chunk = (seq.nk + t.parts - 1) / t.parts, whole = (chunk + kRows - 1) / kRows * kRows;
@@ -83,7 +83,7 @@ __global__ __launch_bounds__((FEW ? kFewWaves<T, D> : 4) * 64, (FEW || (sizeof(T
     const int part_begin = from < seq.nk ? (int)from : seq.nk, begin = part_begin + (FEW ? wave * kRows : 0);
     const int end = min(min(part_begin + whole, seq.nk), visible_of(min(first + (1 << kShift), pairs) - 1));
 
-    const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
+    const Rows gk = {t.ldk, 1, 0, 0, t.head}, gv = {t.ldv, 1, 0, 0, t.head};
     Feed<T, D, kRows, NT, FED, false> feed_k, feed_v;
     feed_k.begin(gk, 0);
     feed_v.begin(gv, 0);
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t)
     const int lane = threadIdx.x & 63;
     const int64_t all = part_place(t, t.parts, 0, 0);
     const uint32_t number = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_head = t.q_rows * t.group;          // below 2^30 in all
-    const int head = number / per_head, pair = number - head * per_head, row = divide(pair, t.group_inverse), its = pair - row * t.group;
+    const int head = number / per_head, pair = number - head * per_head, row = hopa_divide(pair, t.group_inverse, t.group_shift), its = pair - row * t.group;
     if (head >= t.k_heads) return;
     int b = 0, e = t.q_rows;
     if (t.q_begin) {

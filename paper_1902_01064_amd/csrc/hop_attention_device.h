@@ -170,13 +170,12 @@ struct Sums {
 };
 
 // ---- from memory to tiles ---------------------------------------------------------------
-__device__ __forceinline__ int divide(int x, uint32_t inverse) { return (int)(__umulhi((uint32_t)x, inverse) + ((uint32_t)x & (inverse ? 0u : ~0u))); }
-
 // Where the rows of a tile lie: rows of keys, `ld` apart; or pairs, whose group's heads lie beside each other in a row.
 struct Rows {
     int64_t ld;
     int group;
-    uint32_t inverse;
+    uint32_t inverse;                           // of the group, see hopa_divide
+    int shift;
     int cols;
 };
 
@@ -203,19 +202,19 @@ struct Feed {
         rest = rest_;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int l = line(i), c = chunk(i) * L::kChunk, row = PAIRS ? divide(rest + l, g.inverse) : l;
+            const int l = line(i), c = chunk(i) * L::kChunk, row = PAIRS ? hopa_divide(rest + l, g.inverse, g.shift) : l;
             const uint32_t at = (uint32_t)row * (uint32_t)g.ld + (PAIRS ? (rest + l - row * g.group) * g.cols : 0) + c;
             place[i] = FED ? (c >= g.cols ? kOutside : at * (uint32_t)sizeof(T)) : at;
         }
     }
     // rows first, first + 1, ... (numbers of rows, or of pairs), `count` (at least 1) of them exist; base: row 0's first column of the head or the group
     __device__ __forceinline__ void issue(char* stage, const T* base, const Rows& g, int first, int count) {
-        const int row0 = PAIRS ? divide(first, g.inverse) : first;
+        const int row0 = PAIRS ? hopa_divide(first, g.inverse, g.shift) : first;
         if (PAIRS && first - row0 * g.group != rest) begin(g, first - row0 * g.group);
         const T* from = base + row0 * g.ld;
         if (count > ROWS) count = ROWS;
         if constexpr (FED) {
-            const int64_t end = PAIRS ? divide(rest + count - 1, g.inverse) * g.ld + g.group * g.cols : (count - 1) * g.ld + g.cols;
+            const int64_t end = PAIRS ? hopa_divide(rest + count - 1, g.inverse, g.shift) * g.ld + g.group * g.cols : (count - 1) * g.ld + g.cols;
             const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(end * sizeof(T)), 0x00020000);
             const int wave = thread() >> 6;
 #pragma unroll

@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kPlanners) void attention_plan_kernel(HopAttentionT
             if (of_keys) {
                 n = (pairs - min(pairs, seen_from(t, tile.nq, tile.nk, tile.first) / rows * rows) + rows - 1) / rows;
             } else {
-                const int last = divide(min(tile.first + kTile, pairs) - 1, t.group_inverse);
+                const int last = hopa_divide(min(tile.first + kTile, pairs) - 1, t.group_inverse, t.group_shift);
                 n = ((t.causal ? clamp_int(last + 1 + tile.nk - tile.nq, 0, tile.nk) : tile.nk) + rows - 1) / rows;
             }
             if (n < 1) n = 1;                           // it has zeros to write
@@ -180,18 +180,18 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         const Sequence its_rows = {seq.q0, seq.nq, seq.k0, seq.nk};
         const int pairs = seq.nq * t.group, first = seq.first, mine = first + wave * 32, pair = mine + (lane & 31);
         const bool live = pair < pairs;
-        const int row = live ? divide(pair, t.group_inverse) : 0, its = live ? pair - row * t.group : 0;
+        const int row = live ? hopa_divide(pair, t.group_inverse, t.group_shift) : 0, its = live ? pair - row * t.group : 0;
         const int64_t at = seq.q0 + row;
         const int column = (head * t.group + its) * t.cols;
         const T* k = (const T*)t.k + seq.k0 * t.ldk + head * t.head;
         const T* v = (const T*)t.v + seq.k0 * t.ldv + head * t.head;
 
         const int limit = live ? visible(its_rows, t.causal, row) : seq.nk;
-        auto visible_of = [&](int p) { return visible(its_rows, t.causal, divide(p, t.group_inverse)); };
+        auto visible_of = [&](int p) { return visible(its_rows, t.causal, hopa_divide(p, t.group_inverse, t.group_shift)); };
         const int all_see = visible_of(min(mine, pairs - 1)), all_see_here = visible_of(first), some_see = mine < pairs ? visible_of(min(mine + 32, pairs) - 1) : 0;
         const int end = min(visible_of(min(first + kTile, pairs) - 1), last_stage * kRows), begin = first_stage * kRows;
 
-        const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
+        const Rows gk = {t.ldk, 1, 0, 0, t.head}, gv = {t.ldv, 1, 0, 0, t.head};
         Feed<T, D, kRows, NT, true, false> feed_k, feed_v;
         feed_k.begin(gk, 0);
         feed_v.begin(gv, 0);
@@ -202,13 +202,13 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         };
         const int n = begin < end ? (end - begin + kRows - 1) / kRows : 0;
         // The tile's queries, gradients and results come through the buffers of the stages.
-        const Rows gq = {t.ldq, t.group, t.group_inverse, t.head}, gg = {t.ldgrad, t.group, t.group_inverse, t.head}, go = {t.ldo, t.group, t.group_inverse, t.head};
+        const Rows gq = {t.ldq, t.group, t.group_inverse, t.group_shift, t.head}, gg = {t.ldgrad, t.group, t.group_inverse, t.group_shift, t.head}, go = {t.ldo, t.group, t.group_inverse, t.group_shift, t.head};
         Feed<T, D, kTile, NT, true, true> feed;
         typename L::frag fq[kS], fg[kS];
         char* const second = kH == 2 ? pool + kStage : pool;
         const int in_tile = 32 * wave * L::kLine;
         auto fetch_tile = [&](char* to, const void* m, const Rows& g) __attribute__((always_inline)) {
-            feed.begin(g, first - divide(first, t.group_inverse) * t.group);
+            feed.begin(g, first - hopa_divide(first, t.group_inverse, t.group_shift) * t.group);
             feed.issue(to, (const T*)m + seq.q0 * g.ld + head * t.group * t.head, g, first, pairs - first);
         };
         __syncthreads();                                   // with whoever still reads from the buffers
@@ -397,7 +397,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         const int all_see = seen_from(t, seq.nq, seq.nk, min(mine + 32, seq.nk) - 1), all_see_here = seen_from(t, seq.nq, seq.nk, min(first + kTile, seq.nk) - 1);
         const int start = min(pairs, seen_from(t, seq.nq, seq.nk, first) / kRows * kRows);
         const int begin = start + first_stage * kRows, end = min(pairs, start + last_stage * kRows);
-        const Rows gq = {t.ldq, t.group, t.group_inverse, t.head}, gg = {t.ldgrad, t.group, t.group_inverse, t.head};
+        const Rows gq = {t.ldq, t.group, t.group_inverse, t.group_shift, t.head}, gg = {t.ldgrad, t.group, t.group_inverse, t.group_shift, t.head};
         Feed<T, D, kRows, NT, true, true> feed_q, feed_g;
         feed_q.begin(gq, 0);
         feed_g.begin(gg, 0);
@@ -412,7 +412,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             }
         };
         const int n = begin < end ? (end - begin + kRows - 1) / kRows : 0;
-        const Rows gk = {t.ldk, 1, 0, t.head}, gv = {t.ldv, 1, 0, t.head};
+        const Rows gk = {t.ldk, 1, 0, 0, t.head}, gv = {t.ldv, 1, 0, 0, t.head};
         Feed<T, D, kTile, NT, true, false> feed;
         auto fetch_tile = [&](char* to, const void* m, const Rows& g) __attribute__((always_inline)) {
             feed.begin(g, 0);
@@ -610,7 +610,7 @@ __device__ __forceinline__ void join_tile(const HopAttentionTask& t, int most) {
             if constexpr (KEYS) {
                 to = (which ? (T*)t.dv + (seq.k0 + n) * t.lddv : (T*)t.dk + (seq.k0 + n) * t.lddk) + head * t.cols + c;
             } else {
-                const int row = divide(n, t.group_inverse);
+                const int row = hopa_divide(n, t.group_inverse, t.group_shift);
                 to = (T*)t.dq + (int64_t)(seq.q0 + row) * t.lddq + (head * t.group + n - row * t.group) * t.cols + c;
             }
             const float by = which ? 1.f : t.scale;

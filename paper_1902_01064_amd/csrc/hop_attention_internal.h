@@ -14,7 +14,8 @@ struct HopAttentionTask {
     int32_t S, q_rows, k_rows;
     int32_t k_heads, group, cols;          // group: query heads of a key head
     int32_t head;                          // columns from a head to the next one where q, k, v, o and grad are read
-    uint32_t group_inverse;                // ceil(2^32 / group), 0 for 1
+    uint32_t group_inverse;                // see hopa_divide
+    int32_t group_shift;
     int32_t causal, parts;
     float scale, scale_log2;               // scale_log2 = scale log2(e)
     const void *q, *k, *v;
@@ -30,6 +31,20 @@ struct HopAttentionTask {
     float* terms;                          // of every pair, [2][k_heads][q_rows group]: lse log2(e) and sum do o
     void *q_plan, *k_plan;                 // how pairs and keys are shared out
 };
+
+// Pairs' rows: x / group, exact for all x below 2^31.  shift = ceil(log2 group) - 1 and inverse = ceil(2^(32 + shift) / group), below 2^32; rounding it up by e / group, e < group <=
+// 2^(shift + 1), makes the quotient too large by x e / (2^(32 + shift) group) < 1 / group, which never reaches the next whole number.  A group of 1 has no inverse: 0.
+constexpr int32_t hopa_group_shift(int32_t group) {
+    int32_t shift = 0;
+    while (2 << shift < group) ++shift;
+    return shift;
+}
+constexpr uint32_t hopa_group_inverse(int32_t group) {
+    return group == 1 ? 0 : (uint32_t)((((uint64_t)1 << (32 + hopa_group_shift(group))) + group - 1) / group);
+}
+constexpr int hopa_divide(int x, uint32_t inverse, int32_t shift) {
+    return (int)((uint32_t)((uint64_t)(uint32_t)x * inverse >> 32) >> shift) + (int)((uint32_t)x & (inverse ? 0u : ~0u));
+}
 
 // Matrices that are copied first, each to rows of `heads` heads `head` columns apart.
 struct HopAttentionCopies {
