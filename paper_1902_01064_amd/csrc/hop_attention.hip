@@ -132,8 +132,10 @@ __global__ __launch_bounds__((FEW ? kFewWaves<T, D> : 4) * 64, (FEW || (sizeof(T
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, p[u][r]);
         if (__any(__builtin_fmaf(most, t.scale_log2, -8.f) > top)) {
-            // only of columns with such a score, so that a row's bits do not depend on the rows beside it
-            const float its = both_max(most) * t.scale_log2, now = its - 8.f > top ? its : top, by = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
+            // only of columns with such a score, so that a row's bits do not depend on the rows beside it; in front of the first one there is nothing to scale but what
+            // the second pass added by hand, which zero would turn into NaN
+            const float its = both_max(most) * t.scale_log2, now = its - 8.f > top ? its : top;
+            const float by = now == top || top == -kInf ? 1.f : __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= by;
 #pragma unroll
