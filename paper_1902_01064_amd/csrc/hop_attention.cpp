@@ -13,12 +13,11 @@ using namespace hopl;
 namespace {
 
 constexpr int64_t kMostPairs = 1 << 30;         // rows times heads: pairs are counted in 31 bits
-constexpr int64_t kMostDistance = 1 << 22;      // a tile's rows, 64 apart at most, lie within the 31 bits of a buffer's places
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 bool table_ok(const int32_t* begin, int S) { return (begin || S == 1) && ((uintptr_t)begin & 3u) == 0; }
 // a matrix of rows with heads: as matrix_ok, and not too far apart
-bool heads_ok(const void* p, int64_t ld, int64_t cols, size_t elem) { return matrix_ok(p, ld, cols, elem) && ld <= kMostDistance; }
+bool heads_ok(const void* p, int64_t ld, int64_t cols, size_t elem) { return matrix_ok(p, ld, cols, elem) && ld <= kHopaMostDistance; }
 
 bool rotate_ok(const hop_rotate_args* a) {
     if (!a || !groups_ok(a->groups, a->index != nullptr) || !index_ok(a->index, a->groups.G)) return false;

@@ -186,6 +186,7 @@ template <typename T, int D, int ROWS, int NT, bool FED, bool PAIRS>
 struct Feed {
     typedef Tile<T, D> L;
     static constexpr int kLoads = ROWS * L::kPlaces / NT;
+    static_assert(ROWS <= kHopaMostTileRows, "their distance");
     uint32_t place[kLoads];                     // FED: bytes behind the tile's first row; else elements
     typename L::frag held[FED ? 1 : kLoads];
     int rest;

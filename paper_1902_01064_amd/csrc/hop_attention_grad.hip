@@ -20,6 +20,7 @@ using namespace hopa;
 namespace {
 
 constexpr int kShift = 7, kTile = 1 << kShift;          // pairs or keys of a tile, 32 of a wavefront
+static_assert(kTile <= kHopaMostTileRows, "their distance");
 constexpr int kCus = 256;
 // kSkip: units that a wavefront's columns see nothing of are left out in fp32, whose products take long (32 sequences of 128 rows: 99 us, with them 103); in bfloat16 the other
 // wavefronts of the stage decide and the branch costs more than it saves (8192 rows, causal: 1003 us, without it 960).

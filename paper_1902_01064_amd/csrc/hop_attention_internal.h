@@ -7,6 +7,13 @@
 #include "hop_attention.h"
 #include "hop_layers_internal.h"
 
+// A tile's rows lie within the 31 bits of a buffer's places: the gradients' tiles are the largest, 128 rows of keys, or as many pairs, which are that many rows where a
+// group has one head and 65 at most where it has more.
+constexpr int64_t kHopaMostDistance = (int64_t)1 << 22;
+constexpr int kHopaMostTileRows = 128;
+static_assert((kHopaMostTileRows - 1) * kHopaMostDistance * 4 + HOP_MAX_HEAD_COLS * 4 < (int64_t)1 << 31, "rows of a tile");
+static_assert(kHopaMostTileRows / 2 * kHopaMostDistance * 4 + (int64_t)HOP_MAX_HEADS * HOP_MAX_HEAD_COLS * 4 < (int64_t)1 << 31, "pairs of a tile");
+
 // A head of queries and a row are a *pair*; the pairs of a key head's group are numbered row by row, head by head within a row, and the
 // kernels work on runs of pairs: every key and value that is read serves all heads of the group.
 struct HopAttentionTask {
