@@ -24,6 +24,8 @@ static_assert(kTile <= kHopaMostTileRows, "their distance");
 constexpr int kCus = 256;
 // kSkip: units that a wavefront's columns see nothing of are left out in fp32, whose products take long (32 sequences of 128 rows: 99 us, with them 103); in bfloat16 the other
 // wavefronts of the stage decide and the branch costs more than it saves (8192 rows, causal: 1003 us, without it 960).
+template <typename T>
+constexpr bool kSkip = sizeof(T) == 4;
 constexpr int kExact = 128;                             // keys: see attention_dq_kernel
 // Two halves of a workgroup with the same tile take every other 32 rows of a stage, so that a SIMD has two wavefronts, of which one computes while the other waits, and the CU
 // only one set of tiles (one wavefront with twice the registers issues an instruction every 5 cycles at best, which is too few beside its products: 1860 us for the above).  In fp32 with 128 columns the sums and operands of one wavefront fill a SIMD's registers.
@@ -162,7 +164,6 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
     typedef Weights<T> W;
     constexpr int kH = kHalves<T, D>, NT = 256 * kH, kRows = 32 * kH, kBytes = kRows * L::kLine, kU = D / 32, kS = L::kSteps;
     constexpr int kStage = 2 * kBytes;                      // keys, values
-    constexpr bool kSkip = sizeof(T) == 4;
     __shared__ __attribute__((aligned(16))) char pool[2 * kStage];
     __shared__ int not_finite;
     __shared__ float exact[2][kTile];
@@ -275,7 +276,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
         auto work = [&](const char* b, int i) __attribute__((always_inline)) {
             const Places<T, D> places = all_places.again();
             const int key = begin + i * kRows + 32 * half;
-            if (kSkip && key >= some_see) return;                      // all of it is hidden from the wavefront's pairs
+            if (kSkip<T> && key >= some_see) return;                      // all of it is hidden from the wavefront's pairs
             const char* sk = b + 32 * half * L::kLine;
             const char* sv = sk + kBytes;
             constexpr int kN = 2 * kS + 2 * kU, kAhead = sizeof(T) == 4 ? 2 : 4, kFrom = kS + (sizeof(T) == 4 ? 1 : 2);
@@ -364,7 +365,6 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
     typedef Tile<T, D> L;
     typedef Weights<T> W;
     constexpr int kH = kHalves<T, D>, NT = 256 * kH, kRows = 32 * kH, kBytes = kRows * L::kLine, kS = L::kSteps;
-    constexpr bool kSkip = sizeof(T) == 4;
     constexpr int kStage = 2 * kBytes + 512;                // queries, gradients, lse log2(e) of the pairs, their D
     // Both sums of 128 columns leave no registers for the keys and values: there they wait in LDS.
     constexpr bool kHeld = kH == 1 || D * sizeof(T) <= 128;
@@ -449,7 +449,7 @@ __global__ __launch_bounds__((256 * kHalves<T, D>), (kHalves<T, D>)) void attent
             Places<T, D> places = all_places.again();
             if constexpr (kCuts > 1) places.across ^= cut * kSumCols * (int)sizeof(T);
             const int pair = begin + i * kRows + 32 * half;
-            if (kSkip && pair + 32 <= some_see) return;                // all of it is hidden from the wavefront's keys
+            if (kSkip<T> && pair + 32 <= some_see) return;                // all of it is hidden from the wavefront's keys
             const char* sq = b + 32 * half * L::kLine;
             const char* sg = sq + kBytes;
             const char* st = b + 2 * kBytes + 128 * half + 16 * hi;
