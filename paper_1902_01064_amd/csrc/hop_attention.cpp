@@ -129,7 +129,7 @@ int hop_rotate(const hop_rotate_args* a, const void* x, int64_t ldx, void* y, in
 
 size_t hop_rotate_grad_scratch_bytes(const hop_rotate_args* a, const hop_rotate_grads* g) {
     if (!rotate_grads_ok(a, g) || !(g->dq_weight || g->dk_weight)) return 0;
-    return (size_t)hopa_rotate_chunks(a->groups.rows, a->groups.G, a->q_heads + a->k_heads) * 2 * (size_t)a->cols * 4;
+    return (size_t)hopa_rotate_chunks(a->groups.rows, a->groups.G) * 2 * (size_t)a->cols * 4;
 }
 
 int hop_rotate_grad(const hop_rotate_args* a, const hop_rotate_grads* g, void* scratch, size_t scratch_bytes, void* stream) {

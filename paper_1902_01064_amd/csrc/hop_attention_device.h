@@ -180,13 +180,14 @@ struct Rows {
 };
 
 // FED: addresses and distances are multiples of 16 bytes, and so are the heads: the memory unit fills the tile itself, through a buffer descriptor whose end
-// is that of the rows that there are (what lies outside comes back as zero).  Else through registers, by 128-bit loads at an element's address.
+// is that of the rows that there are (what lies outside comes back as zero).  Else, rows of keys only, through registers, by 128-bit loads at an element's address.
 // A lane's places in a tile are worked out once, and for pairs again where a tile begins with another head than the one before.
 template <typename T, int D, int ROWS, int NT, bool FED, bool PAIRS>
 struct Feed {
     typedef Tile<T, D> L;
     static constexpr int kLoads = ROWS * L::kPlaces / NT;
     static_assert(ROWS <= kHopaMostTileRows, "their distance");
+    static_assert(FED || !PAIRS, "pairs come from aligned rows");
     uint32_t place[kLoads];                     // FED: bytes behind the tile's first row; else elements
     typename L::frag held[FED ? 1 : kLoads];
     int rest;

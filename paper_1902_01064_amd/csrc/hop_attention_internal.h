@@ -97,5 +97,14 @@ int hopa_grad(const HopAttentionTask& t, int dtype, const HopAttentionPlan& plan
 
 int hopa_rotate(const HopRotateTask& t, int dtype, const HopIndex& index, void* stream);
 int hopa_rotate_grad(const HopRotateTask& t, int dtype, const HopIndex& index, const HopIndex& dindex, void* stream);
-int hopa_rotate_shift(int64_t rows, int32_t heads);
-int64_t hopa_rotate_chunks(int64_t rows, int G, int32_t heads);
+// The gradient to weights: rows of a chunk, 1 << shift, and how many chunks there are at most.
+constexpr int64_t kHopaMostChunks = 1 << 20;
+inline int hopa_rotate_shift(int64_t rows) {
+    int shift = 0;
+    while ((shift < 6 && (rows >> shift) > 1024) || (rows >> shift) > kHopaMostChunks) ++shift;
+    return shift;
+}
+inline int64_t hopa_rotate_chunks(int64_t rows, int G) {
+    const int shift = hopa_rotate_shift(rows);
+    return ((rows + (1 << shift) - 1) >> shift) + G;
+}

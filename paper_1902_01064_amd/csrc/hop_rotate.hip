@@ -16,8 +16,7 @@ using namespace hopl;
 namespace {
 
 constexpr int NT = 256, kBlock = 4, kMostPairs = HOP_MAX_HEAD_COLS / 2;       // rows whose angles are worked out at once
-constexpr int64_t kMostChunks = 1 << 20;                                       // of a launch
-// Where the other column of a pair is: in the lane half a head away (halves of whole heads of 2^k columns), in the same lane (neighbours), or anywhere.
+// Where the other column of a pair is: in the lane half a head away (halves of whole heads of 2^k columns), in the same lane (neighbours), or anywhere in the head.
 enum { kLanes, kNeighbours, kAnywhere };
 
 struct Shared {
@@ -119,8 +118,8 @@ __device__ __forceinline__ f32x8 turn(const HopRotateTask& t, Shared& sh, f32x8 
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int c = c0 + e;
-            const bool turned = c < t.rotary, first = t.adjacent ? (c & 1) == 0 : c < half;
-            const int i = !turned ? 0 : t.adjacent ? c >> 1 : first ? c : c - half, at = !turned ? c : t.adjacent ? c ^ 1 : first ? c + half : c - half;
+            const bool turned = c < t.rotary, first = c < half;
+            const int i = !turned ? 0 : first ? c : c - half, at = !turned ? c : first ? c + half : c - half;
             other[e] = mine[at];
             cosine[e] = turned ? sh.cosine[r][i] : 1.f;
             sine[e] = turned ? first != back ? -sh.sine[r][i] : sh.sine[r][i] : 0.f;
@@ -357,21 +356,10 @@ void backward(const HopRotateTask& t, const HopIndex& index, unsigned grid, hipS
 
 }  // namespace
 
-int hopa_rotate_shift(int64_t rows, int32_t heads) {
-    (void)heads;
-    int shift = 0;
-    while ((shift < 6 && (rows >> shift) > 1024) || (rows >> shift) > kMostChunks) ++shift;
-    return shift;
-}
-int64_t hopa_rotate_chunks(int64_t rows, int G, int32_t heads) {
-    const int shift = hopa_rotate_shift(rows, heads);
-    return ((rows + (1 << shift) - 1) >> shift) + G;
-}
-
 int hopa_rotate(const HopRotateTask& task, int dtype, const HopIndex& index, void* stream) {
     HopRotateTask t = task;
     t.shift = t.rows.rows > 2048 ? 2 : 0;
-    while ((t.rows.rows >> t.shift) > kMostChunks) ++t.shift;
+    while ((t.rows.rows >> t.shift) > kHopaMostChunks) ++t.shift;
     const unsigned grid = (unsigned)(((int64_t)t.rows.rows + (1 << t.shift) - 1) / (1 << t.shift) + (t.rows.begin ? t.rows.G : 0));
     if (dtype == HOP_BF16) forward<bf16>(t, index, grid, (hipStream_t)stream);
     else forward<float>(t, index, grid, (hipStream_t)stream);
@@ -380,9 +368,9 @@ int hopa_rotate(const HopRotateTask& task, int dtype, const HopIndex& index, voi
 
 int hopa_rotate_grad(const HopRotateTask& task, int dtype, const HopIndex& index, const HopIndex& dindex, void* stream) {
     HopRotateTask t = task;
-    t.shift = hopa_rotate_shift(t.rows.rows, t.heads);
+    t.shift = hopa_rotate_shift(t.rows.rows);
     if (t.rows.rows) {
-        const unsigned grid = (unsigned)hopa_rotate_chunks(t.rows.rows, t.rows.begin ? t.rows.G : 0, t.heads);
+        const unsigned grid = (unsigned)hopa_rotate_chunks(t.rows.rows, t.rows.begin ? t.rows.G : 0);
         if (dtype == HOP_BF16) backward<bf16>(t, index, grid, (hipStream_t)stream);
         else backward<float>(t, index, grid, (hipStream_t)stream);
     }

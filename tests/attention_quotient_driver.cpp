@@ -38,7 +38,6 @@ HopAttentionPlan hopa_grad_plan(HopAttentionTask*, int, char*) { return {}; }
 int hopa_grad(const HopAttentionTask& t, int, const HopAttentionPlan&, void*) { return task_ok(t), 0; }
 int hopa_rotate(const HopRotateTask&, int, const HopIndex&, void*) { return 0; }
 int hopa_rotate_grad(const HopRotateTask&, int, const HopIndex&, const HopIndex&, void*) { return 0; }
-int64_t hopa_rotate_chunks(int64_t rows, int G, int32_t) { return rows + G; }
 
 int main() {
     std::vector<float> room(64);
