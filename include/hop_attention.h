@@ -14,7 +14,7 @@
  *  - A head is `cols` consecutive columns of a row.  Query head h belongs to key head h / (q_heads / k_heads); q_heads is a multiple of k_heads.
  *  - Sequences lie packed in the rows: sequence s has the query rows q_begin[s] to q_begin[s + 1] and the key rows k_begin[s] to k_begin[s + 1],
  *    two tables of S + 1 ascending row numbers on the device (the same one where queries and keys are the same rows).  A sequence may have none of
- *    either.  Rows in front of the first and behind the last sequence are neither read nor written.
+ *    either; so room behind a sequence's keys, where a cache grows, is a sequence without queries.  Rows in front of the first and behind the last sequence are neither read nor written.
  *  - `causal`: the queries are the last rows of their sequence, query i of nq sees the keys up to i + nk - nq of nk.  So one query sees all keys of
  *    its sequence, and with more queries than keys the first ones see none: their o is 0, their lse -infinity, they have no gradient.
  *  - What a query does not see has no influence, whatever it holds: infinities and NaN in keys and values behind a query, or in queries (and
