@@ -316,7 +316,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(HopAttentionTask t)
 bool few(const HopAttentionTask& t) { return (int64_t)t.q_rows * t.group <= (int64_t)32 * t.S; }
 
 // Few queries read a key once, and that is all their time: they fill tiles from rows that are not aligned through registers, and others' rows are copied first.
-// In fp32 tiles of 128 columns and what is on its way to them are more than all registers (172 bytes of scratch a lane), so there rows are copied for few queries too.
+// In fp32 tiles of 128 columns and what is on its way to them are more than all registers (172 bytes of scratch a lane), so there rows are copied for few queries too: the next token
+// of 16 sequences of 8192 tokens, 8 key heads of 128 columns, 361 us, not aligned 793.  In bfloat16 twice as many tokens take 207 us, not aligned, through registers, 248.
 template <typename T, int D>
 constexpr bool kThroughRegisters = D * (int)sizeof(T) <= 256;
 

@@ -40,7 +40,8 @@ __device__ __forceinline__ int seen_from(const HopAttentionTask& t, int nq, int 
 // A workgroup for the tiles of pairs, one for those of keys.  `rows`: of a stage.
 constexpr int kPlanners = 1024;
 // What a tile takes beside its stages, in stages: 17500 cycles for pairs, of which a stage of 128 columns in bfloat16 takes 2440, and more for keys.  12288 tokens, 16 heads on 2:
-// dq and dk, dv in 215 and 237 us; as if a tile took nothing 439 and 272.
+// dq and dk, dv in 215 and 237 us; as if a tile took nothing 439 and 272.  Measured there; fewer columns and fp32 have stages of
+// other lengths and are weighed by the same numbers.
 constexpr int kPairsFixed = 8, kKeysFixed = 10;
 __device__ __forceinline__ int64_t scan_all(int64_t v, int64_t* waves, int64_t* all) {          // sum of those in front
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
